@@ -288,6 +288,120 @@ dc_status dc_tile_dims(const dc_problem* prob, int32_t dims[4]);
 /* Static string for a status code. */
 const char* dc_status_string(int32_t status);
 
+/* ---- between two convolutions: norm, pointwise products, 8-bit checkpoints ---- */
+
+/*
+ * What a network applies between two convolutions of a decomposed layer
+ * (Sec. III-A: these operations need no halo and no other tile): layer norm over
+ * the channels of each pixel, products over the channels (1x1 layers, the
+ * matrices of a feed-forward block) with bias, activation and residual in the
+ * epilogue, and activations kept for the backward pass in 8 bits.  They read and
+ * write tiles where they lie: the fp32 output of a convolution, the interior of
+ * a padded tile, rows of channels.
+ *
+ * A view describes a tensor [N][C][H][W] in memory: element strides of samples,
+ * channels and rows; columns are contiguous.  H = W = 1 with sc = 1 is a matrix
+ * of N rows of C channels, W = 1 with sc = 1 and sh = C one of N H rows.  A
+ * pointer goes with every view: 16-byte aligned for fp32 gamma, beta, bias,
+ * weights, gradients, statistics, checkpoints and workspaces; aligned to its
+ * element for a view (an interior starts anywhere).  What lies in memory between
+ * the first and the last element of a view (margins, the gap after a row) may be
+ * read with it; those values never reach a result.  Strides of tensors that are read may be 0
+ * (broadcast); those of tensors that are written must not make elements overlap
+ * (DC_ERR_SHAPE).  Outputs must not overlap inputs, except where said.
+ * N H W is below 2^31 (DC_ERR_TOO_LARGE); offsets are 64-bit.
+ */
+#define DC_Q8 2   /* view dtype: a checkpoint in 8 bits (layout below, strides ignored) */
+typedef struct {
+    int32_t N, C, H, W;
+    int64_t sn, sc, sh;    /* element strides: sample, channel, row */
+    int32_t dtype;         /* DC_F32, DC_BF16 or DC_Q8 */
+} dc_view;
+
+typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_GELU = 2, DC_ACT_SILU = 3 } dc_activation;
+
+/*
+ * The 8-bit form of a tensor: the 32 channels 32k .. 32k+31 of a pixel are a
+ * block and share a scale byte s, the biased fp32 exponent of their largest
+ * magnitude, at least 7.  A value is q * 2^(s-133), q the nearest integer (ties
+ * to even) within -127 .. 127: the error is at most 2^-7 of the block's power of
+ * two (2^-6 at its very top), and every value is exact in bf16.  A block with an
+ * infinity or NaN has s = 255 and stands for NaN throughout.
+ * Layout: q [N][ceil(C/32)][H W][32] int8, then s [N][ceil(C/32)][H W]; channels
+ * past C hold q = 0.  dc_ckpt_bytes() is the total, a multiple of 16; -1 for an
+ * invalid view.
+ */
+int64_t dc_ckpt_bytes(const dc_view* vq);
+
+/* x (fp32 or bf16) -> its 8-bit form q (dc_ckpt_bytes of the same N, C, H, W). */
+dc_status dc_ckpt_save(const dc_view* vx, const void* x, void* q, void* stream);
+
+/* y = act(what q stands for), y fp32 or bf16. */
+dc_status dc_ckpt_load(const dc_view* vq, const void* q, int32_t act, const dc_view* vy, void* y,
+                       void* stream);
+
+/*
+ * Layer norm of each pixel over its C channels, in fp32 with the variance from
+ * centred values:  u = gamma (x - mu) r + beta,  mu = mean x,  r = (var x +
+ * eps)^-1/2.  gamma and beta are fp32 [C]; either may be NULL (1 and 0).
+ * stat [2][N][H][W] (mu, then r) and ckpt (x in 8 bits) are written unless NULL;
+ * the backward pass reads stat, and x or its checkpoint.  u may be x itself
+ * (same view and type).
+ */
+dc_status dc_norm_fwd(const dc_view* vx, const void* x, const float* gamma, const float* beta, float eps,
+                      const dc_view* vu, void* u, float* stat, void* ckpt, void* stream);
+
+/*
+ * Its backward pass: with xh = (x - mu) r and g = gamma du,
+ *   dx = r (g - mean g - xh mean(g xh)) [+ res],
+ *   dgamma (=|+=) sum over pixels of du xh,  dbeta (=|+=) sum over pixels of du.
+ * x is the forward's input, or its checkpoint where vx->dtype is DC_Q8; stat is
+ * what the forward wrote.  res (a skip path's gradient), u (gamma xh + beta once
+ * more, for a weight gradient that reads it), dgamma and dbeta may be NULL; beta
+ * is read for u only.  dx may be du or res (same view and type).  accumulate = 0
+ * overwrites dgamma and dbeta, 1 adds to them.  workspace: device scratch of at
+ * least dc_norm_bwd_workspace_bytes(vdu) bytes.  The summation order is fixed.
+ */
+dc_status dc_norm_bwd(const dc_view* vdu, const void* du, const dc_view* vx, const void* x, const float* stat,
+                      const float* gamma, const float* beta, const dc_view* vres, const void* res,
+                      const dc_view* vu, void* u, const dc_view* vdx, void* dx, float* dgamma, float* dbeta,
+                      int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+size_t dc_norm_bwd_workspace_bytes(const dc_view* vdu);
+
+/*
+ * Product over the channels of every pixel:  z = W x + bias,  y = act(z) + res.
+ * w is [K][C] with K = vy->C and C = vx->C, of x's type; bias fp32 [K] or NULL;
+ * res (fp32 or bf16) or NULL; z is written too unless NULL, whole (fp32, bf16) or
+ * in 8 bits (vz->dtype DC_Q8), for dc_linear_bwd_data.  y is fp32 or bf16 and may
+ * be res (same view and type).  bf16 products are exact, fp32 ones fp32; sums are
+ * fp32 in a fixed order.
+ */
+dc_status dc_linear_fwd(const dc_view* vx, const void* x, const void* w, const float* bias, int32_t act,
+                        const dc_view* vres, const void* res, const dc_view* vz, void* z,
+                        const dc_view* vy, void* y, void* stream);
+
+/*
+ * Gradient at what an activation read, from the gradient dy of the product after
+ * it:  dx = (W^T dy) act'(z),  w [K][C] of dy's type, K = vdy->C, C = vdx->C.  z
+ * (whole or DC_Q8) is read unless act is DC_ACT_NONE, where dx is the plain input
+ * gradient and vz, z, vh and h are NULL.  h = act(z) is written unless NULL: the
+ * product's input again, for its weight gradient.
+ */
+dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, int32_t act,
+                             const dc_view* vz, const void* z, const dc_view* vh, void* h,
+                             const dc_view* vdx, void* dx, void* stream);
+
+/*
+ * Weight and bias gradient of a product:  dw[k][c] (=|+=) sum over pixels of
+ * dy[k] x[c],  db[k] (=|+=) sum over pixels of dy[k];  db may be NULL.  x and dy
+ * are of one type.  workspace: at least dc_linear_bwd_filter_workspace_bytes()
+ * bytes (0: none).  The summation order is fixed.
+ */
+dc_status dc_linear_bwd_filter(const dc_view* vx, const void* x, const dc_view* vdy, const void* dy,
+                               float* dw, float* db, int32_t accumulate, void* workspace,
+                               size_t workspace_bytes, void* stream);
+size_t dc_linear_bwd_filter_workspace_bytes(const dc_view* vx, const dc_view* vdy);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,6 +33,9 @@ DC_X, DC_DY = 0, 1
 DC_ALL_TILES = -1
 DC_BAND_NS, DC_BAND_WE, DC_BAND_CORNERS, DC_BAND_ALL = 1, 2, 4, 7
 DC_REGION_ALL, DC_REGION_INTERIOR, DC_REGION_BOUNDARY = 0, 1, 2
+DC_Q8 = 2   # view dtype: an activation checkpoint in 8 bits
+DC_ACT_NONE, DC_ACT_RELU, DC_ACT_GELU, DC_ACT_SILU = 0, 1, 2, 3
+ACT = {"none": DC_ACT_NONE, "relu": DC_ACT_RELU, "gelu": DC_ACT_GELU, "silu": DC_ACT_SILU}
 # capacity of the fixed workspace of dc_conv_bwd_filter_noalloc (include/dc.h)
 BWD_FILTER_NOALLOC_MAX_BYTES = 64 << 20
 
@@ -48,6 +51,8 @@ EXPORTS = (
     "dc_conv_fwd_region", "dc_conv_bwd_data_region", "dc_validate",
     "dc_tile_pitch", "dc_tile_elems", "dc_halo_elems", "dc_bwd_filter_workspace_bytes",
     "dc_required_halo", "dc_halo_bands", "dc_tile_dims", "dc_status_string",
+    "dc_ckpt_bytes", "dc_ckpt_save", "dc_ckpt_load", "dc_norm_fwd", "dc_norm_bwd", "dc_norm_bwd_workspace_bytes",
+    "dc_linear_fwd", "dc_linear_bwd_data", "dc_linear_bwd_filter", "dc_linear_bwd_filter_workspace_bytes",
 )
 
 
@@ -64,6 +69,34 @@ class Problem(ctypes.Structure):
             dt = {"f32": DC_F32, "bf16": DC_BF16}[dt]
         return cls(layer.N, layer.C, layer.K, layer.H, layer.W, layer.R, layer.S,
                    layer.stride, layer.pad, layer.P, layer.Q, layer.halo, dt)
+
+
+_VIEW_DT = {torch.float32: DC_F32, torch.bfloat16: DC_BF16}
+
+
+class View(ctypes.Structure):
+    """``dc_view``: a tensor [N][C][H][W] in memory, columns contiguous.
+
+    Built once per layout (``of`` a tensor, ``q8`` for a checkpoint) and passed
+    beside the tensor it describes.
+    """
+    _fields_ = ([(n, ctypes.c_int32) for n in ("N", "C", "H", "W")] +
+                [(n, ctypes.c_int64) for n in ("sn", "sc", "sh")] + [("dtype", ctypes.c_int32)])
+
+    @classmethod
+    def of(cls, t) -> "View":
+        """Of a 4-D fp32 or bf16 tensor, or slice of one, whose columns are contiguous."""
+        if t.dim() != 4 or t.dtype not in _VIEW_DT:
+            raise ValueError(f"a view describes a 4-D float32 or bfloat16 tensor, not {t.dim()}-D {t.dtype}")
+        (n, c, h, w), (sn, sc, sh, sw) = t.shape, t.stride()
+        if sw != 1 and w > 1:
+            raise ValueError(f"a view's columns are contiguous: got a column stride of {sw}")
+        return cls(n, c, h, w, sn, sc, sh, _VIEW_DT[t.dtype])
+
+    @classmethod
+    def q8(cls, N, C, H, W) -> "View":
+        """Of the 8-bit checkpoint of such a tensor (a buffer of ckpt_bytes)."""
+        return cls(N, C, H, W, 0, 0, 0, DC_Q8)
 
 
 class DcError(RuntimeError):
@@ -100,6 +133,24 @@ _lib.dc_required_halo.argtypes = [_P, _I, ctypes.POINTER(_I)]
 _lib.dc_tile_dims.argtypes = [_P, ctypes.POINTER(_I)]
 _lib.dc_status_string.argtypes = [_I]
 _lib.dc_status_string.restype = ctypes.c_char_p
+_W = ctypes.POINTER(View)
+_Z = ctypes.c_size_t
+_lib.dc_ckpt_bytes.argtypes = [_W]
+_lib.dc_ckpt_bytes.restype = ctypes.c_int64
+_lib.dc_ckpt_save.argtypes = [_W, _V, _V, _V]
+_lib.dc_ckpt_load.argtypes = [_W, _V, _I, _W, _V, _V]
+_lib.dc_norm_fwd.argtypes = [_W, _V, _V, _V, ctypes.c_float, _W, _V, _V, _V, _V]
+_lib.dc_norm_bwd.argtypes = [_W, _V, _W, _V, _V, _V, _V, _W, _V, _W, _V, _W, _V, _V, _V, _I, _V, _Z, _V]
+_lib.dc_norm_bwd_workspace_bytes.argtypes = [_W]
+_lib.dc_norm_bwd_workspace_bytes.restype = _Z
+_lib.dc_linear_fwd.argtypes = [_W, _V, _V, _V, _I, _W, _V, _W, _V, _W, _V, _V]
+_lib.dc_linear_bwd_data.argtypes = [_W, _V, _V, _I, _W, _V, _W, _V, _W, _V, _V]
+_lib.dc_linear_bwd_filter.argtypes = [_W, _V, _W, _V, _V, _V, _I, _V, _Z, _V]
+_lib.dc_linear_bwd_filter_workspace_bytes.argtypes = [_W, _W]
+_lib.dc_linear_bwd_filter_workspace_bytes.restype = _Z
+for _n in ("dc_ckpt_save", "dc_ckpt_load", "dc_norm_fwd", "dc_norm_bwd", "dc_linear_fwd", "dc_linear_bwd_data",
+           "dc_linear_bwd_filter"):
+    getattr(_lib, _n).restype = ctypes.c_int32
 for _n in ("dc_conv_fwd", "dc_conv_bwd_data", "dc_conv_bwd_filter", "dc_conv_bwd_filter_noalloc",
            "dc_halo_pack", "dc_halo_unpack", "dc_halo_pack_bands", "dc_halo_unpack_bands",
            "dc_conv_fwd_region", "dc_conv_bwd_data_region",
@@ -254,3 +305,73 @@ def conv_bwd_data_region(prob, tile, region, dy_pad, w, dx, stream=None):
     """Eq. (3) on the interior (no halo read) or the boundary frame of a tile."""
     _check(_lib.dc_conv_bwd_data_region(ctypes.byref(prob), tile, region, _ptr(dy_pad), _ptr(w),
                                         _ptr(dx), _stream(stream)), "dc_conv_bwd_data_region")
+
+
+# ------------------------------------- between two convolutions (views: View)
+
+def _view(v):
+    return None if v is None else ctypes.byref(v)
+
+
+def _bytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def ckpt_bytes(vq):
+    """Bytes of the 8-bit checkpoint of a tensor of vq's N, C, H, W; -1 if invalid."""
+    return _lib.dc_ckpt_bytes(ctypes.byref(vq))
+
+
+def ckpt_save(vx, x, q, stream=None):
+    """q <- x in 8 bits."""
+    _check(_lib.dc_ckpt_save(_view(vx), _ptr(x), _ptr(q), _stream(stream)), "dc_ckpt_save")
+
+
+def ckpt_load(vq, q, act, vy, y, stream=None):
+    """y <- act(what q stands for)."""
+    _check(_lib.dc_ckpt_load(_view(vq), _ptr(q), act, _view(vy), _ptr(y), _stream(stream)), "dc_ckpt_load")
+
+
+def norm_fwd(vx, x, gamma, beta, eps, vu, u, stat=None, ckpt=None, stream=None):
+    """u <- layer norm of each pixel of x over its channels; stat (mean, 1/deviation) and
+    ckpt (x in 8 bits) for the backward pass."""
+    _check(_lib.dc_norm_fwd(_view(vx), _ptr(x), _ptr(gamma), _ptr(beta), eps, _view(vu), _ptr(u), _ptr(stat),
+                            _ptr(ckpt), _stream(stream)), "dc_norm_fwd")
+
+
+def norm_bwd_workspace_bytes(vdu):
+    return _lib.dc_norm_bwd_workspace_bytes(ctypes.byref(vdu))
+
+
+def norm_bwd(vdu, du, vx, x, stat, gamma, beta, vres, res, vu, u, vdx, dx, dgamma, dbeta, accumulate, workspace,
+             stream=None):
+    """dx <- input gradient of norm_fwd (+ res), dgamma, dbeta (=|+=) the parameters'; x is the
+    input or its checkpoint (vx of dtype DC_Q8).  res, u (the forward's output again), dgamma and
+    dbeta may be None."""
+    _check(_lib.dc_norm_bwd(_view(vdu), _ptr(du), _view(vx), _ptr(x), _ptr(stat), _ptr(gamma), _ptr(beta),
+                            _view(vres), _ptr(res), _view(vu), _ptr(u), _view(vdx), _ptr(dx), _ptr(dgamma),
+                            _ptr(dbeta), accumulate, _ptr(workspace), _bytes(workspace), _stream(stream)),
+           "dc_norm_bwd")
+
+
+def linear_fwd(vx, x, w, bias, act, vres, res, vz, z, vy, y, stream=None):
+    """y <- act(w x + bias) + res over the channels of every pixel; z (whole or 8-bit) keeps what
+    act reads.  bias, res and z may be None."""
+    _check(_lib.dc_linear_fwd(_view(vx), _ptr(x), _ptr(w), _ptr(bias), act, _view(vres), _ptr(res), _view(vz),
+                              _ptr(z), _view(vy), _ptr(y), _stream(stream)), "dc_linear_fwd")
+
+
+def linear_bwd_data(vdy, dy, w, act, vz, z, vh, h, vdx, dx, stream=None):
+    """dx <- (w^T dy) act'(z); h <- act(z) again unless None.  act DC_ACT_NONE: z and h are None."""
+    _check(_lib.dc_linear_bwd_data(_view(vdy), _ptr(dy), _ptr(w), act, _view(vz), _ptr(z), _view(vh), _ptr(h),
+                                   _view(vdx), _ptr(dx), _stream(stream)), "dc_linear_bwd_data")
+
+
+def linear_bwd_filter_workspace_bytes(vx, vdy):
+    return _lib.dc_linear_bwd_filter_workspace_bytes(ctypes.byref(vx), ctypes.byref(vdy))
+
+
+def linear_bwd_filter(vx, x, vdy, dy, dw, db, accumulate, workspace, stream=None):
+    """dw (=|+=) sum over pixels of dy x^T, db (=|+=) sum over pixels of dy (or None)."""
+    _check(_lib.dc_linear_bwd_filter(_view(vx), _ptr(x), _view(vdy), _ptr(dy), _ptr(dw), _ptr(db), accumulate,
+                                     _ptr(workspace), _bytes(workspace), _stream(stream)), "dc_linear_bwd_filter")

@@ -1,0 +1,271 @@
+// What the kernels between two convolutions (norm, pointwise products, 8-bit
+// checkpoints) share: views of tiles, pixel numbering, activations, the 8-bit form.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include <cstdint>
+
+#include "dc.h"
+
+namespace dc {
+
+// n / d for n < 2^31 by the host's m = ceil(2^(31+l) / d), l = ceil(log2 d): the
+// error of m adds less than n 2^l / (d 2^(31+l)) < 1 / d to the quotient.
+// m = 0 stands for d = 1.
+struct FastDiv {
+    uint32_t m, sh, d;
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return m ? __umulhi(n, m) >> sh : n; }
+};
+
+inline FastDiv fast_div(uint32_t d) {
+    FastDiv f{0, 0, d};
+    if (d > 1) {
+        int l = 0;
+        while ((uint64_t(1) << l) < d) ++l;
+        f.m = uint32_t(((uint64_t(1) << (31 + l)) + d - 1) / d);
+        f.sh = uint32_t(l - 1);
+    }
+    return f;
+}
+
+// A view on the device: pointer, element strides, type.
+struct View {
+    char* p;
+    int64_t sn, sc, sh;
+    int32_t dt;        // DC_F32, DC_BF16, DC_Q8; -1: absent
+};
+
+// The pixels of a set of views, numbered sample by sample in rows of `len`: the
+// tile's rows, or all of an image as one row where every view's rows follow each
+// other without a gap (then sh is never used).
+struct Pixels {
+    int32_t M;         // N H W
+    int32_t HW, len;
+    FastDiv dHW, dlen;
+};
+
+// 8-bit form: q at 32 bytes per pixel and block, scales behind (one byte each)
+struct Q8Map {
+    int64_t qn, s0, sn;   // bytes per sample of q; start and bytes per sample of the scales
+    int32_t HW;
+};
+inline Q8Map q8_map(int64_t N, int C, int64_t HW) {
+    const int64_t cb = (C + 31) / 32;
+    return Q8Map{cb * HW * 32, N * cb * HW * 32, cb * HW, int32_t(HW)};
+}
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// one element; bf16 widens exactly
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const __bf16* p) {
+    return __builtin_bit_cast(float, uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
+}
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__bf16* p, float v) { *p = static_cast<__bf16>(v); }   // nearest, ties to even
+
+// ---- activations, formed in fp32.
+//
+// gelu is z Phi(z) with the normal distribution's Phi; its slope Phi(z) + z phi(z).
+// Phi's tail is phi-like, so one exponential serves both: for a = |z| / sqrt 2,
+// erfc(a) = t (a1 + t (a2 + ...)) e^(-a^2), t = 1 / (1 + p a), with the
+// coefficients of Abramowitz and Stegun, Handbook of Mathematical Functions
+// (1964), 7.1.26: |error| <= 1.5e-7, a rounding of fp32 near 1.
+struct Phi { float cdf, pdf; };
+__device__ __forceinline__ Phi normal(float z) {
+    const float a = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.0f));
+    const float e = __expf(-a * a);
+    float s = fmaf(1.061405429f, t, -1.453152027f);
+    s = fmaf(s, t, 1.421413741f);
+    s = fmaf(s, t, -0.284496736f);
+    s = fmaf(s, t, 0.254829592f);
+    const float tail = 0.5f * s * t * e;       // Phi(-|z|)
+    return Phi{z < 0 ? tail : 1.0f - tail, 0.39894228040143268f * e};
+}
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_fwd(float z) {
+    if constexpr (ACT == DC_ACT_RELU) return z <= 0 ? 0.0f : z;   // NaN stays
+    if constexpr (ACT == DC_ACT_GELU) return z * normal(z).cdf;
+    if constexpr (ACT == DC_ACT_SILU) return z * logistic(z);
+    return z;
+}
+
+// value and slope at once
+template <int ACT>
+__device__ __forceinline__ void act_both(float z, float& v, float& d) {
+    if constexpr (ACT == DC_ACT_RELU) {
+        v = z <= 0 ? 0.0f : z;
+        d = z <= 0 ? 0.0f : z > 0 ? 1.0f : z;
+    } else if constexpr (ACT == DC_ACT_GELU) {
+        const Phi n = normal(z);
+        v = z * n.cdf;
+        d = fmaf(z, n.pdf, n.cdf);
+    } else if constexpr (ACT == DC_ACT_SILU) {
+        const float s = logistic(z);
+        v = z * s;
+        d = fmaf(v, 1.0f - s, s);
+    } else {
+        v = z;
+        d = 1.0f;
+    }
+}
+
+// ---- the 8-bit form
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+// scale byte of a block whose largest magnitude has these bits (as integers they
+// order like the magnitudes, NaN above infinity)
+__device__ __forceinline__ uint32_t q8_scale(uint32_t top) { return max(top >> 23, 7u); }
+__device__ __forceinline__ float q8_per(uint32_t s) { return __builtin_bit_cast(float, (260u - s) << 23); }
+__device__ __forceinline__ float q8_step(uint32_t s) {
+    return __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : (s - 6u) << 23);
+}
+// four values -> four bytes, lowest first.  per is a power of two: the products
+// are exact, and the one rounding is rint's.  The block of a NaN may hold any q.
+__device__ __forceinline__ int q8_of(float v, float per) {
+    return int(fminf(fmaxf(__builtin_rintf(v * per), -127.0f), 127.0f));
+}
+__device__ __forceinline__ uint32_t q8_pack(float a, float b, float c, float d, float per) {
+    const uint32_t lo = (uint32_t(q8_of(a, per)) & 0xffu) | (uint32_t(q8_of(b, per)) & 0xffu) << 8;
+    const uint32_t hi = (uint32_t(q8_of(c, per)) & 0xffu) | (uint32_t(q8_of(d, per)) & 0xffu) << 8;
+    return lo | hi << 16;
+}
+// byte k of w as a value
+__device__ __forceinline__ float q8_value(uint32_t w, int k, float step) {
+    return float(int32_t(w << (24 - 8 * k)) >> 24) * step;
+}
+
+// Where pixel m of the numbering lies.
+struct Pixel { int n, h, w, pix; };
+__device__ __forceinline__ Pixel pixel_of(const Pixels& x, int m) {
+    Pixel r;
+    r.n = int(x.dHW.div(uint32_t(m)));
+    r.pix = m - r.n * x.HW;
+    r.h = int(x.dlen.div(uint32_t(r.pix)));
+    r.w = r.pix - r.h * x.len;
+    return r;
+}
+
+// The lane's address of a pixel in a view.
+template <typename T>
+__device__ __forceinline__ char* spot_of(const View& v, const Pixel& p) {
+    return v.p + (p.n * v.sn + p.h * v.sh + p.w) * int64_t(sizeof(T));
+}
+// The next channel's address.  Kept from the optimiser, which would otherwise form the
+// offsets of 32 channels of every tensor ahead of a loop and run out of registers (2.5 KB
+// of scratch a lane in the norm's backward pass).
+__device__ __forceinline__ void next(char*& p, int64_t step) {
+    p += step;
+    asm("" : "+v"(p));
+}
+
+// Values of one pixel's block of 32 channels (first: c0), loaded and stored.  CL: the
+// channels are contiguous and lie on 16-byte boundaries (host check: C, the
+// strides and the base), so a block is whole 16-byte vectors; else every channel
+// is an access of its own, contiguous over the wave's pixels.
+template <typename T, bool CL>
+__device__ __forceinline__ void load_block(float (&v)[32], const View& t, const Pixel& p, int c0, int C) {
+    char* a = spot_of<T>(t, p) + c0 * (CL ? 1 : t.sc) * int64_t(sizeof(T));
+    if constexpr (CL) {
+        constexpr int VE = 16 / int(sizeof(T));
+#pragma unroll
+        for (int j = 0; j < 32 / VE; ++j) {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (c0 + j * VE < C) u = *reinterpret_cast<const uint4*>(a + j * 16);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                if constexpr (VE == 4)
+                    v[j * VE + i] = __builtin_bit_cast(float, w[i]);
+                else
+                    v[j * VE + i] = __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+            }
+        }
+    } else {
+        const int64_t step = t.sc * int64_t(sizeof(T));
+        if (c0 + 32 <= C) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, next(a, step)) v[j] = load1(reinterpret_cast<const T*>(a));
+        } else {      // channels past C count as zero
+#pragma unroll
+            for (int j = 0; j < 32; ++j, next(a, step)) {
+                v[j] = 0;
+                if (c0 + j < C) v[j] = load1(reinterpret_cast<const T*>(a));
+            }
+        }
+    }
+}
+
+template <typename T, bool CL>
+__device__ __forceinline__ void store_block(const View& t, const Pixel& p, int c0, int C, const float (&v)[32]) {
+    char* a = spot_of<T>(t, p) + c0 * (CL ? 1 : t.sc) * int64_t(sizeof(T));
+    if constexpr (CL) {
+        constexpr int VE = 16 / int(sizeof(T));
+#pragma unroll
+        for (int j = 0; j < 32 / VE; ++j) {
+            if (c0 + j * VE >= C) continue;
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (VE == 4)
+                    w[i] = __builtin_bit_cast(uint32_t, v[j * VE + i]);
+                else
+                    w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                                                            (f32x2_t{v[j * VE + 2 * i], v[j * VE + 2 * i + 1]}), bf16x2_t));
+            }
+            *reinterpret_cast<uint4*>(a + j * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    } else {
+        const int64_t step = t.sc * int64_t(sizeof(T));
+        if (c0 + 32 <= C) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, next(a, step)) store1(reinterpret_cast<T*>(a), v[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j, next(a, step))
+                if (c0 + j < C) store1(reinterpret_cast<T*>(a), v[j]);
+        }
+    }
+}
+
+// a block's bytes and scale <-> its values
+__device__ __forceinline__ void q8_store_block(char* q, const Q8Map& m, const Pixel& p, int cb, const float (&v)[32]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) top = max(top, abs_bits(v[j]));
+    const uint32_t s = q8_scale(top);
+    const float per = q8_per(s);
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = q8_pack(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3], per);
+    const uint32_t at = uint32_t(cb) * uint32_t(m.HW) + uint32_t(p.pix);
+    uint4* d = reinterpret_cast<uint4*>(q + p.n * m.qn + int64_t(at) * 32);
+    d[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    d[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    reinterpret_cast<uint8_t*>(q)[m.s0 + p.n * m.sn + at] = uint8_t(s);
+}
+
+__device__ __forceinline__ void q8_load_block(float (&v)[32], const char* q, const Q8Map& m, const Pixel& p, int cb) {
+    const uint32_t at = uint32_t(cb) * uint32_t(m.HW) + uint32_t(p.pix);
+    const uint4* d = reinterpret_cast<const uint4*>(q + p.n * m.qn + int64_t(at) * 32);
+    const uint4 a = d[0], b = d[1];
+    const float step = q8_step(reinterpret_cast<const uint8_t*>(q)[m.s0 + p.n * m.sn + at]);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = q8_value(w[j / 4], j % 4, step);
+}
+
+// Workgroup index with each of the 8 XCDs (round-robin dispatch) on a contiguous
+// range, so that neighbours share their XCD's L2; total is the grid.
+__device__ __forceinline__ int xcd_range(int b, int total) {
+    const int per = total / 8, rest = total % 8, x = b % 8, i = b / 8;
+    return x * per + min(x, rest) + i;
+}
+
+}  // namespace dc

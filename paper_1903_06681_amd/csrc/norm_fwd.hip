@@ -1,0 +1,96 @@
+// Layer norm over the channels of each pixel, forward.
+//
+//   u = gamma (x - mu) r + beta,  mu = mean x,  r = (mean (x - mu)^2 + eps)^-1/2
+//
+// Bound: memory (about ten operations per value).  A lane holds one pixel's block
+// of 32 channels in registers: every channel's access is contiguous over the
+// wave's pixels, the sums over channels are the lane's own plus one exchange
+// through LDS with the other blocks of the pixel, and the 8-bit form's scale needs
+// no exchange at all.  One pass over the data: the variance comes from the
+// centred registers, not from a difference of large sums.
+#include <algorithm>
+
+#include "norm.h"
+
+namespace dc {
+
+template <typename XT, int LPX, int R, bool CL>
+__global__ __launch_bounds__(512) void norm_fwd_kernel(NormArgs a) {
+    __shared__ float red[2][1][kNormWaves * LPX];
+    const NormLane l = norm_lane<LPX>(a);
+    const int m = (xcd_range(blockIdx.x, a.grid) * a.pg + l.pg) * LPX + l.px;
+    const bool in = m < a.px.M;
+    const Pixel p = pixel_of(a.px, min(m, a.px.M - 1));
+    float v[R ? R : 1][32];
+    float s[1] = {0};
+    each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
+        load_block<XT, CL>(v[i], a.x, p, cb * 32, a.C);
+    });
+    each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
+        if constexpr (!R) load_block<XT, CL>(v[0], a.x, p, cb * 32, a.C);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) s[0] += v[i][j];
+    });
+    pixel_sum<LPX>(s, a, l, red[0]);
+    const float mu = s[0] * a.invC;
+    s[0] = 0;
+    each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
+        if constexpr (!R) load_block<XT, CL>(v[0], a.x, p, cb * 32, a.C);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float d = cb * 32 + j < a.C ? v[i][j] - mu : 0.0f;
+            s[0] = fmaf(d, d, s[0]);
+        }
+    });
+    pixel_sum<LPX>(s, a, l, red[1]);
+    const float r = 1.0f / sqrtf(s[0] * a.invC + a.eps);
+    if (!in) return;
+    if (a.stat && l.unit == 0) {
+        a.stat[m] = mu;
+        a.stat[int64_t(a.px.M) + m] = r;
+    }
+    each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
+        if constexpr (!R) load_block<XT, CL>(v[0], a.x, p, cb * 32, a.C);
+        if (a.q) q8_store_block(a.q, a.qm, p, cb, v[i]);
+        float g[32], b[32];
+        load_params(g, a.gamma, cb * 32, a.C, 1.0f);
+        load_params(b, a.beta, cb * 32, a.C, 0.0f);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) g[j] = fmaf(g[j], (v[i][j] - mu) * r, b[j]);
+        store_any<CL>(a.u, p, cb * 32, a.C, g);
+    });
+}
+
+// Which pixels and blocks go side by side.  Rows of channels (cl): the lanes of a
+// pixel lie next to each other, so that a wave reads whole rows.  Else 64 pixels
+// a wave, or 16 where that leaves the chip without work (fewer than 2048 waves of
+// 64 pixels and 32 channels) or the channels do not fit a workgroup's registers.
+bool norm_plan(NormArgs& a, bool backward) {
+    a.blocks = (a.C + 31) / 32;
+    a.invC = 1.0f / float(a.C);
+    const int64_t waves = (int64_t(a.px.M) + 63) / 64 * a.blocks;
+    if (a.cl)
+        a.lpx = a.blocks >= 16 ? 4 : 16;
+    else
+        a.lpx = a.blocks <= 2 * kNormWaves && waves >= 2048 ? 64 : 16;
+    const int sb = 64 / a.lpx;
+    a.nw = std::min((a.blocks + sb - 1) / sb, kNormWaves);
+    const int held = (a.blocks + a.nw * sb - 1) / (a.nw * sb);
+    a.held = held <= 1 ? 1 : held == 2 && !a.cl ? 2 : 0;
+    a.groups = int((int64_t(a.px.M) + a.lpx - 1) / a.lpx);
+    // enough workgroups for the chip first, then up to eight waves each
+    a.pg = std::max(1, std::min(kNormWaves / a.nw, a.groups / 512));
+    a.grid = (a.groups + a.pg - 1) / a.pg;
+    if (backward) a.grid = std::min(a.grid, 512);   // two workgroups a compute unit
+    return true;
+}
+
+hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s) {
+    if (a.x.dt == DC_F32)
+        DC_NORM_LAUNCH(norm_fwd_kernel, a, s, float);
+    else
+        DC_NORM_LAUNCH(norm_fwd_kernel, a, s, __bf16);
+    return hipGetLastError();
+}
+
+}  // namespace dc
