@@ -74,25 +74,27 @@ __device__ __forceinline__ void store1(__bf16* p, float v) { *p = static_cast<__
 // Phi's tail is phi-like, so one exponential serves both: for a = |z| / sqrt 2,
 // erfc(a) = t (a1 + t (a2 + ...)) e^(-a^2), t = 1 / (1 + p a), with the
 // coefficients of Abramowitz and Stegun, Handbook of Mathematical Functions
-// (1964), 7.1.26: |error| <= 1.5e-7, a rounding of fp32 near 1.
-struct Phi { float cdf, pdf; };
-__device__ __forceinline__ Phi normal(float z) {
-    const float a = fabsf(z) * 0.70710678118654752f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.0f));
-    const float e = __expf(-a * a);
-    float s = fmaf(1.061405429f, t, -1.453152027f);
-    s = fmaf(s, t, 1.421413741f);
-    s = fmaf(s, t, -0.284496736f);
-    s = fmaf(s, t, 0.254829592f);
-    const float tail = 0.5f * s * t * e;       // Phi(-|z|)
-    return Phi{z < 0 ? tail : 1.0f - tail, 0.39894228040143268f * e};
+// (1964), 7.1.26 (here halved, p over sqrt 2): |error| <= 1.5e-7, a rounding of fp32
+// near 1.  Twenty issue slots a value, eight of them the exponential and the
+// reciprocal: an epilogue's vector operations weigh as much as its matrix ones.
+struct Normal { float tail, e; };   // Phi(-|z|), e^(-z^2 / 2)
+__device__ __forceinline__ Normal normal(float z) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.23164189f, 1.0f));
+    const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    float s = fmaf(0.5307027145f, t, -0.7265760135f);
+    s = fmaf(s, t, 0.7107068705f);
+    s = fmaf(s, t, -0.142248368f);
+    s = fmaf(s, t, 0.127414796f);
+    return Normal{s * t * e, e};
 }
-__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+__device__ __forceinline__ float logistic(float z) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+}
 
 template <int ACT>
 __device__ __forceinline__ float act_fwd(float z) {
     if constexpr (ACT == DC_ACT_RELU) return z <= 0 ? 0.0f : z;   // NaN stays
-    if constexpr (ACT == DC_ACT_GELU) return z * normal(z).cdf;
+    if constexpr (ACT == DC_ACT_GELU) return fmaxf(z, 0.0f) - fabsf(z) * normal(z).tail;
     if constexpr (ACT == DC_ACT_SILU) return z * logistic(z);
     return z;
 }
@@ -104,9 +106,9 @@ __device__ __forceinline__ void act_both(float z, float& v, float& d) {
         v = z <= 0 ? 0.0f : z;
         d = z <= 0 ? 0.0f : z > 0 ? 1.0f : z;
     } else if constexpr (ACT == DC_ACT_GELU) {
-        const Phi n = normal(z);
-        v = z * n.cdf;
-        d = fmaf(z, n.pdf, n.cdf);
+        const Normal n = normal(z);
+        v = fmaxf(z, 0.0f) - fabsf(z) * n.tail;
+        d = fmaf(z * 0.39894228f, n.e, z < 0 ? n.tail : 1.0f - n.tail);
     } else if constexpr (ACT == DC_ACT_SILU) {
         const float s = logistic(z);
         v = z * s;
@@ -126,15 +128,17 @@ __device__ __forceinline__ float q8_per(uint32_t s) { return __builtin_bit_cast(
 __device__ __forceinline__ float q8_step(uint32_t s) {
     return __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : (s - 6u) << 23);
 }
-// four values -> four bytes, lowest first.  per is a power of two: the products
-// are exact, and the one rounding is rint's.  The block of a NaN may hold any q.
-__device__ __forceinline__ int q8_of(float v, float per) {
-    return int(fminf(fmaxf(__builtin_rintf(v * per), -127.0f), 127.0f));
+// four values -> four bytes, lowest first.  per is a power of two, so v per is exact
+// and 1.5 2^23 + v per rounds to an integer, ties to even, whose low byte is q's.  The
+// block of a NaN may hold any q.
+__device__ __forceinline__ uint32_t q8_bits(float v, float per) {
+    constexpr float kInt = 12582912.0f;
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(fmaf(v, per, kInt), kInt - 127.0f, kInt + 127.0f));
 }
 __device__ __forceinline__ uint32_t q8_pack(float a, float b, float c, float d, float per) {
-    const uint32_t lo = (uint32_t(q8_of(a, per)) & 0xffu) | (uint32_t(q8_of(b, per)) & 0xffu) << 8;
-    const uint32_t hi = (uint32_t(q8_of(c, per)) & 0xffu) | (uint32_t(q8_of(d, per)) & 0xffu) << 8;
-    return lo | hi << 16;
+    const uint32_t lo = __builtin_amdgcn_perm(q8_bits(b, per), q8_bits(a, per), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(q8_bits(d, per), q8_bits(c, per), 0x0c0c0400u);
+    return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
 }
 // byte k of w as a value
 __device__ __forceinline__ float q8_value(uint32_t w, int k, float step) {

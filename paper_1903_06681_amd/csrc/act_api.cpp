@@ -138,6 +138,17 @@ static Operand pixel_operand(const dc_view& v, const void* p) {
     return o;
 }
 
+// Whether every chunk that holds elements of a pixel operand is an aligned 16-byte vector
+// whose elements lie between the view's first and last: rows start on 16-byte
+// boundaries, and either end there or are not the view's last.
+static bool direct_pixels(const dc_view& v, const void* p, bool cl, int64_t row) {
+    const int e = 16 / esize(v);
+    if (misaligned(p)) return false;
+    if ((v.N > 1 && v.sn % e) || (v.H > 1 && v.sh % e && row == v.W)) return false;
+    if (cl) return v.C % e == 0 && (v.H == 1 || v.sh % e == 0);
+    return v.sc % e == 0 && row % e == 0;
+}
+
 static dc_status block_limits(int64_t K, int64_t C, const Slots& s) {
     if (K * C > (int64_t(1) << 31) - 1) return DC_ERR_TOO_LARGE;
     const int64_t slots = int64_t(s.chunks) * s.per, rows = std::max(K, C);
@@ -160,6 +171,7 @@ static dc_status wgrad_args(const dc_view* vx, const dc_view* vdy, const void* x
     a->b = pixel_operand(*vx, x);
     a->a.rows = a->K;
     a->b.rows = a->C;
+    a->direct = direct_pixels(*vx, x, a->cl, a->s.len) && direct_pixels(*vdy, dy, a->cl, a->s.len);
     linear_wgrad_plan(*a, f32);
     return DC_OK;
 }
@@ -328,6 +340,7 @@ dc_status dc_linear_fwd(const dc_view* vx, const void* x, const void* w, const f
     a.b = pixel_operand(*vx, x);
     a.a.rows = a.rows = vy->C;
     a.a.red = a.b.red = vx->C;
+    a.direct = direct_pixels(*vx, x, a.cl, a.s.len) && vx->C % (f32 ? 4 : 8) == 0;
     a.bias = bias;
     a.res = device_view(vres, res);
     a.z = device_view(vz, z);
@@ -372,6 +385,7 @@ dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, 
     a.b = pixel_operand(*vdy, dy);
     a.a.rows = a.rows = vdx->C;
     a.a.red = a.b.red = vdy->C;
+    a.direct = direct_pixels(*vdy, dy, a.cl, a.s.len) && vdx->C % (f32 ? 4 : 8) == 0;
     a.res.dt = -1;
     a.z = device_view(vz, z);
     a.h = device_view(vh, h);

@@ -59,6 +59,7 @@ struct LinearArgs {
     Q8Map qm;
     int32_t rows;          // channels of the result
     int32_t act, cl;       // cl: rows of channels
+    int32_t direct;        // operands on 16-byte boundaries
     int32_t tr, tc;        // blocks along rows and columns
 };
 hipError_t launch_linear_fwd(const LinearArgs& a, bool f32, hipStream_t s);
@@ -73,6 +74,7 @@ struct LinWgradArgs {
     int32_t tr, tc;        // blocks of the result
     int32_t shares, per;   // shares of the slices, slices of a share
     int32_t accumulate, cl;
+    int32_t direct;        // operands on 16-byte boundaries, rows of whole chunks
 };
 void linear_wgrad_plan(LinWgradArgs& a, bool f32);
 size_t linear_wgrad_part_bytes(const LinWgradArgs& a);

@@ -53,53 +53,158 @@ __device__ __forceinline__ void q8_load_half(float (&v)[16], const char* q, cons
     for (int r = 0; r < 16; ++r) v[r] = q8_value(w[r / 4], r % 4, step);
 }
 
-// A lane's 16 channels of one pixel in a view; rows: channels of the view.
-// `whole`: the block lies inside them.
-template <typename T>
-__device__ __forceinline__ void load_half(float (&v)[16], const View& t, int64_t at, int o0, int h, int rows) {
-    const T* p = reinterpret_cast<const T*>(t.p) + at;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = load1(p + min(o0 + 8 * (r / 4) + 4 * h + r % 4, rows - 1) * t.sc);
+// ---- a lane's 16 channels of one pixel in memory
+//
+// Four lanes hold four neighbouring pixels of the same channels.  In bf16 they trade, so
+// that each has one channel of all four: 8 bytes an access instead of 2, a quarter of
+// the accesses (512 -> 2048 channels on 65536 pixels: with 2-byte stores of 268 MB the
+// forward pass took longer than with 4-byte ones of 537 MB).  fp32 goes channel by
+// channel: 128 contiguous bytes a half wave.
+
+// [lane q] (a0 a1 | a2 a3) -> (lane 0's aq, lane 1's aq | lane 2's aq, lane 3's aq)
+__device__ __forceinline__ void trade(uint32_t& lo, uint32_t& hi, int lane) {
+    constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E;      // quad permutations [1 0 3 2], [2 3 0 1]
+    const uint32_t sel = lane & 1 ? 0x03020706u : 0x05040100u;
+    const bool up = lane & 2;
+    const uint32_t e0 = __builtin_amdgcn_perm(__builtin_amdgcn_mov_dpp(lo, kSwap1, 0xf, 0xf, true), lo, sel);
+    const uint32_t e1 = __builtin_amdgcn_perm(__builtin_amdgcn_mov_dpp(hi, kSwap1, 0xf, 0xf, true), hi, sel);
+    const uint32_t got = __builtin_amdgcn_mov_dpp(up ? e0 : e1, kSwap2, 0xf, 0xf, true);
+    lo = up ? got : e0;
+    hi = up ? e1 : got;
 }
-__device__ __forceinline__ void load_half(float (&v)[16], const View& t, int64_t at, int o0, int h, int rows) {
-    if (t.dt == DC_F32)
-        load_half<float>(v, t, at, o0, h, rows);
-    else
-        load_half<__bf16>(v, t, at, o0, h, rows);
+
+// Where a lane's pixel lies, and the first of its four: element offset of a view's
+// channel 0 (the lane's is in range on every lane); pixels from there on in the row.
+struct Place {
+    Chunk c;
+    int w, w4, ok, left4;
+    __device__ __forceinline__ int64_t at(const View& t) const { return c.n * t.sn + c.r * t.sh + w; }
+    __device__ __forceinline__ int64_t at4(const View& t) const { return c.n * t.sn + c.r * t.sh + w4; }
+};
+template <int PER>
+__device__ __forceinline__ Place place_of(const Slots& s, int slot) {
+    Place p;
+    const int sub = slot % PER, sub4 = PER == 1 ? 0 : sub & ~3;
+    p.c = chunk_of(s, slot / PER);
+    p.ok = sub < p.c.left;
+    p.w = p.ok ? p.c.col + sub : 0;
+    p.left4 = p.c.left - sub4;
+    p.w4 = p.left4 > 0 ? p.c.col + sub4 : 0;
+    return p;
 }
-template <typename T>
-__device__ __forceinline__ void store_half(const float (&v)[16], const View& t, int64_t at, int o0, int h, int rows) {
-    T* p = reinterpret_cast<T*>(t.p) + at;
-    if (t.sc == 1 && o0 + 32 <= rows) {      // rows of channels: four lie together
-        typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+// PER: slots of a chunk; 1: rows of channels, which trade nothing.  All lanes call.
+template <typename T, int PER>
+__device__ __forceinline__ void load_half(float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
+    const int h = lane >> 5;
+    const int64_t step = t.sc * int64_t(sizeof(T));
+    if constexpr (PER > 1 && sizeof(T) == 2) {
+        const int q = lane & 3;
+        const char* a = t.p + (p.at4(t) + (o0 + 4 * h + q) * t.sc) * 2;
+        const bool all = p.left4 >= 4;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            T w[4];
+        for (int g = 0; g < 4; ++g, a += 8 * step) {
+            uint32_t lo = 0, hi = 0;
+            if (o0 + 8 * g + 4 * h + q < rows) {
+                if (all) {
+                    const u32x2_any d = *reinterpret_cast<const u32x2_any*>(a);
+                    lo = d.x;
+                    hi = d.y;
+                } else {
+                    const uint16_t* e = reinterpret_cast<const uint16_t*>(a);
+                    if (p.left4 > 0) lo = e[0];
+                    if (p.left4 > 1) lo |= uint32_t(e[1]) << 16;
+                    if (p.left4 > 2) hi = e[2];
+                }
+            }
+            trade(lo, hi, lane);
+            v[4 * g] = __builtin_bit_cast(float, lo << 16);
+            v[4 * g + 1] = __builtin_bit_cast(float, lo & 0xffff0000u);
+            v[4 * g + 2] = __builtin_bit_cast(float, hi << 16);
+            v[4 * g + 3] = __builtin_bit_cast(float, hi & 0xffff0000u);
+        }
+    } else {
+        char* a = t.p + (p.at(t) + (o0 + 4 * h) * t.sc) * int64_t(sizeof(T));
+        const int64_t skip = 5 * step;
+        if (o0 + 32 <= rows) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) store1(w + i, v[4 * g + i]);
-            if constexpr (sizeof(T) == 4) {
-                u32x4_any d;
-                __builtin_memcpy(&d, w, 16);
-                *reinterpret_cast<u32x4_any*>(p + o0 + 8 * g + 4 * h) = d;
-            } else {
-                u32x2_any d;
-                __builtin_memcpy(&d, w, 8);
-                *reinterpret_cast<u32x2_any*>(p + o0 + 8 * g + 4 * h) = d;
+            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) v[r] = load1(reinterpret_cast<const T*>(a));
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) {
+                v[r] = 0;
+                if (o0 + 8 * (r / 4) + 4 * h + r % 4 < rows) v[r] = load1(reinterpret_cast<const T*>(a));
             }
         }
-        return;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int o = o0 + 8 * (r / 4) + 4 * h + r % 4;
-        if (o < rows) store1(p + o * t.sc, v[r]);
     }
 }
-__device__ __forceinline__ void store_half(const float (&v)[16], const View& t, int64_t at, int o0, int h, int rows) {
+template <int PER>
+__device__ __forceinline__ void load_half(float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
     if (t.dt == DC_F32)
-        store_half<float>(v, t, at, o0, h, rows);
+        load_half<float, PER>(v, t, p, o0, lane, rows);
     else
-        store_half<__bf16>(v, t, at, o0, h, rows);
+        load_half<__bf16, PER>(v, t, p, o0, lane, rows);
+}
+
+template <typename T, int PER>
+__device__ __forceinline__ void store_half(const float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
+    const int h = lane >> 5;
+    const int64_t step = t.sc * int64_t(sizeof(T));
+    auto packed = [&](int r) __attribute__((always_inline)) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{v[r], v[r + 1]}), bf16x2_t));
+    };
+    if constexpr (PER > 1 && sizeof(T) == 2) {
+        const int q = lane & 3;
+        char* a = t.p + (p.at4(t) + (o0 + 4 * h + q) * t.sc) * 2;
+        const bool all = p.left4 >= 4;
+#pragma unroll
+        for (int g = 0; g < 4; ++g, a += 8 * step) {
+            uint32_t lo = packed(4 * g), hi = packed(4 * g + 2);
+            trade(lo, hi, lane);
+            if (o0 + 8 * g + 4 * h + q >= rows) continue;
+            if (all) {
+                *reinterpret_cast<u32x2_any*>(a) = u32x2_any{lo, hi};
+            } else {
+                uint16_t* e = reinterpret_cast<uint16_t*>(a);
+                if (p.left4 > 0) e[0] = uint16_t(lo);
+                if (p.left4 > 1) e[1] = uint16_t(lo >> 16);
+                if (p.left4 > 2) e[2] = uint16_t(hi);
+            }
+        }
+    } else {
+        if (!p.ok) return;
+        char* a = t.p + (p.at(t) + (o0 + 4 * h) * t.sc) * int64_t(sizeof(T));
+        if (PER == 1 && t.sc == 1 && o0 + 32 <= rows) {      // rows of channels: four lie together
+#pragma unroll
+            for (int g = 0; g < 4; ++g, a += 8 * sizeof(T)) {
+                if constexpr (sizeof(T) == 4)
+                    *reinterpret_cast<u32x4_any*>(a) =
+                        u32x4_any{__builtin_bit_cast(uint32_t, v[4 * g]), __builtin_bit_cast(uint32_t, v[4 * g + 1]),
+                                  __builtin_bit_cast(uint32_t, v[4 * g + 2]), __builtin_bit_cast(uint32_t, v[4 * g + 3])};
+                else
+                    *reinterpret_cast<u32x2_any*>(a) = u32x2_any{packed(4 * g), packed(4 * g + 2)};
+            }
+            return;
+        }
+        const int64_t skip = 5 * step;
+        if (o0 + 32 <= rows) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) store1(reinterpret_cast<T*>(a), v[r]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip))
+                if (o0 + 8 * (r / 4) + 4 * h + r % 4 < rows) store1(reinterpret_cast<T*>(a), v[r]);
+        }
+    }
+}
+template <int PER>
+__device__ __forceinline__ void store_half(const float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
+    if (t.dt == DC_F32)
+        store_half<float, PER>(v, t, p, o0, lane, rows);
+    else
+        store_half<__bf16, PER>(v, t, p, o0, lane, rows);
 }
 
 template <int N>
@@ -140,117 +245,128 @@ __device__ __forceinline__ void apply_slope(float (&z)[N], float (&v)[N], int ac
     }
 }
 
+// A lane's 16 channels (first of the block: o0) of slot `slot`, summed up: what is
+// left to do and to store.
+template <bool BWD, int PER>
+__device__ __forceinline__ void epilogue(float (&v)[16], const LinearArgs& a, int slot, int o0, int lane) {
+    const Place p = place_of<PER>(a.s, slot);
+    const int pix = p.c.r * a.s.len + p.w, h = lane >> 5;
+    if constexpr (BWD) {
+        if (a.act != DC_ACT_NONE) {
+            float z[16];
+            if (a.z.dt == DC_Q8)
+                q8_load_half(z, a.z.p, a.qm, p.c.n, o0 / 32, pix, h);
+            else
+                load_half<PER>(z, a.z, p, o0, lane, a.rows);
+            apply_slope(z, v, a.act);
+            if (a.h.dt >= 0) store_half<PER>(z, a.h, p, o0, lane, a.rows);
+        }
+    } else {
+        if (a.z.dt == DC_Q8) {
+            if (o0 + 32 > a.rows) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (o0 + 8 * (r / 4) + 4 * h + r % 4 >= a.rows) v[r] = 0;
+            }
+            q8_store_half(a.z.p, a.qm, p.c.n, o0 / 32, pix, p.ok, h, v);
+        } else if (a.z.dt >= 0) {
+            store_half<PER>(v, a.z, p, o0, lane, a.rows);
+        }
+        apply_act(v, a.act);
+        if (a.res.dt >= 0) {
+            float e[16];
+            load_half<PER>(e, a.res, p, o0, lane, a.rows);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) v[r] += e[r];
+        }
+    }
+    store_half<PER>(v, a.out, p, o0, lane, a.rows);
+}
+
 // BWD: the input gradient (weights KR), else the forward pass (weights RK).
-// CL: pixels RK (rows of channels), else KR.
-template <typename T, bool BWD, bool CL, int BM, int BN>
-__global__ __launch_bounds__(kLinThreads) void linear_kernel(LinearArgs a) {
-    constexpr int AK = BWD ? KR : RK, PK = CL ? RK : KR;
-    typedef Stage<T, AK, WEIGHT, BM> SA;
-    typedef Stage<T, PK, PIXEL, BN> SB;
-    constexpr int TM = BM / 64, TN = BN / 64, BK = SA::BK;
-    __shared__ __align__(16) char lds[2][SA::BYTES + SB::BYTES];
+// CL: pixels RK (rows of channels), else KR.  DIRECT: operands on 16-byte boundaries.
+template <typename S, bool BWD, bool CL, bool DIRECT>
+__global__ __launch_bounds__(S::TH, 2) void linear_kernel(LinearArgs a) {
+    typedef typename S::T T;
+    constexpr int AK = BWD ? KR : RK, PK = CL ? RK : KR, TM = S::TM, TN = S::TN;
+    __shared__ __align__(16) char lds[DIRECT ? S::NST : 2][S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // blocks of one column range follow each other on an XCD: they read the same pixels
     const int id = xcd_range(blockIdx.x, a.tr * a.tc);
     const int tc = id / a.tr, tr = id - tc * a.tr;
-    SA sa;
-    SB sb;
-    sa.init(a.a, a.s, tr * BM);
-    sb.init(a.b, a.s, tc * BN);
-    uint4 va[SA::U], vb[SB::U];
+    Stage<T, AK, WEIGHT, S::BM, S::ROWB, S::TH> sa;
+    Stage<T, PK, PIXEL, S::BN, S::ROWB, S::TH> sb;
+    sa.init(a.a, a.s, tr * S::BM);
+    sb.init(a.b, a.s, tc * S::BN);
     f32x16_t acc[TM][TN];
+    const int row0 = wave / S::WN * (32 * TM), col0 = wave % S::WN * (32 * TN), h = lane >> 5;
+    // the sums start from the bias
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+        for (int r = 0; r < 16; ++r) {
+            const int o = min(tr * S::BM + row0 + 32 * i + 8 * (r / 4) + 4 * h + r % 4, a.rows - 1);
+            const float b = !BWD && a.bias ? a.bias[o] : 0.0f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-    const int row0 = (wave >> 1) * (BM / 2), col0 = (wave & 1) * (BN / 2);
-    sa.load(va, a.a, 0);
-    sb.load(vb, a.b, 0);
-    sa.store(va, lds[0]);
-    sb.store(vb, lds[0] + SA::BYTES);
-    __syncthreads();
-    const int red = a.a.red;
-    for (int k = 0, buf = 0; k < red; k += BK, buf ^= 1) {
-        const bool more = k + BK < red;
-        if (more) {
-            sa.load(va, a.a, k + BK);
-            sb.load(vb, a.b, k + BK);
+            for (int j = 0; j < TN; ++j) acc[i][j][r] = b;
         }
-        slice<T, AK, PK, BM, BN, TM, TN>(acc, lds[buf], lds[buf] + SA::BYTES, row0, col0, lane, [](int, const uint4&) {});
-        if (more) {
-            sa.store(va, lds[buf ^ 1]);
-            sb.store(vb, lds[buf ^ 1] + SA::BYTES);
-        }
-        __syncthreads();
-    }
+    tile_loop<S, AK, PK, DIRECT>(acc, sa, sb, a.a, a.b, a.s, 0, a.a.red, lds, row0, col0, lane, [](int, const uint4&) {});
 
-    const int h = lane >> 5;
+    // The blocks of 32 x 32 pass through the wave's share of LDS, a lane's values back to
+    // the lane: a loop at run time instead of one copy of the epilogue per block, which
+    // overran the registers and the instruction cache.
+    constexpr int Q = TM * TN, ROOM = (DIRECT ? S::NST : 2) * S::BYTES / (S::TH * 64), PER = Q < ROOM ? Q : ROOM;
+    char* mine = &lds[0][0] + wave * (PER * 4096) + lane * 16;
+    __syncthreads();
+    static_for<0, (Q + PER - 1) / PER>([&](auto part) __attribute__((always_inline)) {
+        constexpr int q0 = decltype(part)::value * PER, q1 = q0 + PER < Q ? q0 + PER : Q;
+        static_for<q0, q1>([&](auto qc) __attribute__((always_inline)) {
+            constexpr int q = decltype(qc)::value;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-        const int slot = tc * BN + col0 + 32 * j + (lane & 31);
-        const int per = CL ? 1 : SB::E, sub = CL ? 0 : slot % SB::E;
-        const Chunk c = chunk_of(a.s, slot / per);
-        const bool ok = sub < c.left;
-        const int w = ok ? c.col + sub : 0, pix = c.r * a.s.len + w;   // in range on every lane
-        auto at = [&](const View& t) __attribute__((always_inline)) { return c.n * t.sn + c.r * t.sh + w; };
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const int o0 = tr * BM + row0 + 32 * i;
+            for (int g = 0; g < 4; ++g) {
+                const f32x16_t& t = acc[q % TM][q / TM];
+                *reinterpret_cast<f32x4_t*>(mine + (q - q0) * 4096 + g * 1024) =
+                    f32x4_t{t[4 * g], t[4 * g + 1], t[4 * g + 2], t[4 * g + 3]};
+            }
+        });
+#pragma unroll 1
+        for (int q = q0; q < q1; ++q) {
+            const int o0 = tr * S::BM + row0 + 32 * (q % TM);
             if (o0 >= a.rows) continue;
             float v[16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) v[r] = acc[i][j][r];
-            if constexpr (BWD) {
-                if (a.act != DC_ACT_NONE) {
-                    float z[16];
-                    if (a.z.dt == DC_Q8)
-                        q8_load_half(z, a.z.p, a.qm, c.n, o0 / 32, pix, h);
-                    else
-                        load_half(z, a.z, at(a.z), o0, h, a.rows);
-                    apply_slope(z, v, a.act);
-                    if (a.h.dt >= 0 && ok) store_half(z, a.h, at(a.h), o0, h, a.rows);
-                }
-            } else {
-                if (a.bias) {
+            for (int g = 0; g < 4; ++g) {
+                const f32x4_t t = *reinterpret_cast<const f32x4_t*>(mine + (q - q0) * 4096 + g * 1024);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) v[r] += a.bias[min(o0 + 8 * (r / 4) + 4 * h + r % 4, a.rows - 1)];
-                }
-                if (a.z.dt == DC_Q8) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (o0 + 8 * (r / 4) + 4 * h + r % 4 >= a.rows) v[r] = 0;
-                    q8_store_half(a.z.p, a.qm, c.n, o0 / 32, pix, ok, h, v);
-                } else if (a.z.dt >= 0 && ok) {
-                    store_half(v, a.z, at(a.z), o0, h, a.rows);
-                }
-                apply_act(v, a.act);
-                if (a.res.dt >= 0) {
-                    float e[16];
-                    load_half(e, a.res, at(a.res), o0, h, a.rows);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) v[r] += e[r];
-                }
+                for (int r = 0; r < 4; ++r) v[4 * g + r] = t[r];
             }
-            if (ok) store_half(v, a.out, at(a.out), o0, h, a.rows);
+            epilogue<BWD, CL ? 1 : S::E>(v, a, tc * S::BN + col0 + 32 * (q / TM) + (lane & 31), o0, lane);
         }
-    }
+    });
 }
 
-// Blocks of 128 x 128, or of 64 x 64 where those would not fill the chip.
+// Blocks of 128 channels x 256 pixels, or of 64 x 64 where those would not fill the chip.
+template <typename T> using Big = Shape<T, 128, 256, 64, 3, 2, 2>;
+template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2>;
+
+template <typename S, bool BWD>
+static void launch_shape(LinearArgs a, hipStream_t s) {
+    a.tr = (a.rows + S::BM - 1) / S::BM;
+    a.tc = int((int64_t(a.s.chunks) * a.s.per + S::BN - 1) / S::BN);
+    const dim3 g(unsigned(a.tr) * unsigned(a.tc)), t(S::TH);
+    if (a.cl && a.direct) hipLaunchKernelGGL((linear_kernel<S, BWD, true, true>), g, t, 0, s, a);
+    else if (a.cl) hipLaunchKernelGGL((linear_kernel<S, BWD, true, false>), g, t, 0, s, a);
+    else if (a.direct) hipLaunchKernelGGL((linear_kernel<S, BWD, false, true>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((linear_kernel<S, BWD, false, false>), g, t, 0, s, a);
+}
+
 template <typename T, bool BWD>
-static hipError_t launch_linear(LinearArgs a, hipStream_t s) {
+static hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
     const int64_t slots = int64_t(a.s.chunks) * a.s.per;
-    auto blocks = [&](int b) { return ((a.rows + b - 1) / b) * ((slots + b - 1) / b); };
-    const int b = blocks(128) >= 512 ? 128 : 64;
-    a.tr = (a.rows + b - 1) / b;
-    a.tc = int((slots + b - 1) / b);
-    const dim3 g(unsigned(a.tr) * unsigned(a.tc)), t(kLinThreads);
-    if (a.cl && b == 128) hipLaunchKernelGGL((linear_kernel<T, BWD, true, 128, 128>), g, t, 0, s, a);
-    else if (a.cl) hipLaunchKernelGGL((linear_kernel<T, BWD, true, 64, 64>), g, t, 0, s, a);
-    else if (b == 128) hipLaunchKernelGGL((linear_kernel<T, BWD, false, 128, 128>), g, t, 0, s, a);
-    else hipLaunchKernelGGL((linear_kernel<T, BWD, false, 64, 64>), g, t, 0, s, a);
+    if (int64_t((a.rows + 127) / 128) * ((slots + 255) / 256) >= 512)
+        launch_shape<Big<T>, BWD>(a, s);
+    else
+        launch_shape<Small<T>, BWD>(a, s);
     return hipGetLastError();
 }
 

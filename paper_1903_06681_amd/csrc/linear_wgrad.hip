@@ -26,24 +26,21 @@ __device__ __forceinline__ float sum16(const uint4& f) {
     return s;
 }
 
-template <typename T, bool CL, int BM, int BN>
-__global__ __launch_bounds__(kLinThreads) void linear_wgrad_kernel(LinWgradArgs a) {
-    constexpr int KIND = CL ? KR : RK;
-    typedef StagePix<T, KIND, BM> SA;
-    typedef StagePix<T, KIND, BN> SB;
-    constexpr int TM = BM / 64, TN = BN / 64, BK = SA::BK;
-    __shared__ __align__(16) char lds[2][SA::BYTES + SB::BYTES];
+template <typename S, bool CL, bool DIRECT>
+__global__ __launch_bounds__(S::TH, 2) void linear_wgrad_kernel(LinWgradArgs a) {
+    typedef typename S::T T;
+    constexpr int KIND = CL ? KR : RK, TM = S::TM, TN = S::TN;
+    __shared__ __align__(16) char lds[DIRECT ? S::NST : 2][S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int blocks = a.tr * a.tc;
     // the blocks of a share follow each other on an XCD: they read the same pixels
     const int id = xcd_range(blockIdx.x, blocks * a.shares);
     const int share = id / blocks, blk = id - share * blocks;
     const int tr = blk / a.tc, tc = blk - tr * a.tc;
-    SA sa;
-    SB sb;
-    sa.init(a.a, tr * BM);
-    sb.init(a.b, tc * BN);
-    uint4 va[SA::U], vb[SB::U];
+    Stage<T, KIND, LONG, S::BM, S::ROWB, S::TH> sa;
+    Stage<T, KIND, LONG, S::BN, S::ROWB, S::TH> sb;
+    sa.init(a.a, a.s, tr * S::BM);
+    sb.init(a.b, a.s, tc * S::BN);
     f32x16_t acc[TM][TN];
     float bsum[TM];
 #pragma unroll
@@ -54,31 +51,13 @@ __global__ __launch_bounds__(kLinThreads) void linear_wgrad_kernel(LinWgradArgs 
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
     }
-    const int row0 = (wave >> 1) * (BM / 2), col0 = (wave & 1) * (BN / 2);
-    const bool bias = a.db && tc == 0 && (wave & 1) == 0;
-    const int slots = a.s.chunks * a.s.per;
-    const int k0 = share * a.per * BK, k1 = min(slots, k0 + a.per * BK);
-    sa.load(va, a.a, a.s, k0);
-    sb.load(vb, a.b, a.s, k0);
-    sa.store(va, lds[0]);
-    sb.store(vb, lds[0] + SA::BYTES);
-    __syncthreads();
-    for (int k = k0, buf = 0; k < k1; k += BK, buf ^= 1) {
-        const bool more = k + BK < k1;
-        if (more) {
-            sa.load(va, a.a, a.s, k + BK);
-            sb.load(vb, a.b, a.s, k + BK);
-        }
-        slice<T, KIND, KIND, BM, BN, TM, TN>(acc, lds[buf], lds[buf] + SA::BYTES, row0, col0, lane,
-                                             [&](int i, const uint4& f) __attribute__((always_inline)) {
-                                                 if (bias) bsum[i] += sum16<T>(f);
-                                             });
-        if (more) {
-            sa.store(va, lds[buf ^ 1]);
-            sb.store(vb, lds[buf ^ 1] + SA::BYTES);
-        }
-        __syncthreads();
-    }
+    const int row0 = wave / S::WN * (32 * TM), col0 = wave % S::WN * (32 * TN);
+    const bool bias = a.db && tc == 0 && wave % S::WN == 0;
+    const int k0 = share * a.per * S::BK, k1 = min(a.s.chunks * a.s.per, k0 + a.per * S::BK);
+    tile_loop<S, KIND, KIND, DIRECT>(acc, sa, sb, a.a, a.b, a.s, k0, k1, lds, row0, col0, lane,
+                                     [&](int i, const uint4& f) __attribute__((always_inline)) {
+                                         if (bias) bsum[i] += sum16<T>(f);
+                                     });
 
     const int h = lane >> 5;
     const bool last = a.shares == 1;
@@ -87,10 +66,10 @@ __global__ __launch_bounds__(kLinThreads) void linear_wgrad_kernel(LinWgradArgs 
     const bool add = last && a.accumulate;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const int o0 = tr * BM + row0 + 32 * i;
+        const int o0 = tr * S::BM + row0 + 32 * i;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            const int c = tc * BN + col0 + 32 * j + (lane & 31);
+            const int c = tc * S::BN + col0 + 32 * j + (lane & 31);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int o = o0 + 8 * (r / 4) + 4 * h + r % 4;
@@ -108,56 +87,69 @@ __global__ __launch_bounds__(kLinThreads) void linear_wgrad_kernel(LinWgradArgs 
     }
 }
 
-// sums of the shares in order; the last row of the result is db
+// The sums of the shares, in a fixed order: 64 results a workgroup, its four waves a
+// quarter of the shares each.  The last K results are db.
 __global__ __launch_bounds__(256) void linear_wgrad_sum_kernel(LinWgradArgs a) {
+    __shared__ float red[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t n = int64_t(a.K) * a.C, all = n + (a.db ? a.K : 0);
-    const int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (e >= all) return;
-    const bool bias = e >= n;
+    const int64_t e = int64_t(blockIdx.x) * 64 + lane;
+    const bool in = e < all, bias = e >= n;
     const float* p = bias ? a.part + a.shares * n + (e - n) : a.part + e;
     const int64_t step = bias ? a.K : n;
+    const int per = (a.shares + 3) / 4, i1 = min((wave + 1) * per, a.shares);
     float s = 0;
-    for (int i = 0; i < a.shares; ++i) s += p[i * step];
+#pragma unroll 8
+    for (int i = wave * per; i < i1; ++i) s += in ? p[i * step] : 0.0f;
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || !in) return;
+    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
     float* d = bias ? a.db + (e - n) : a.dw + e;
     *d = a.accumulate ? *d + s : s;
 }
 
-// Blocks of 128 x 128, or of 64 x 64 for small results; shares so that about 512
-// workgroups run, none with fewer than four slices.
-static int block_of(const LinWgradArgs& a) { return a.K > 64 && a.C > 64 ? 128 : 64; }
+// Blocks of 128 x 256, or of 64 x 64 for small results; shares so that about 512
+// workgroups run, none with fewer than four slices of 128 bytes.
+template <typename T> using Big = Shape<T, 128, 256, 64, 3, 2, 2>;
+template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2>;
+static bool big(const LinWgradArgs& a) { return a.K > 64 && a.C > 128; }
 
-void linear_wgrad_plan(LinWgradArgs& a, bool f32) {
-    const int b = block_of(a), bk = f32 ? 32 : 64;
-    a.tr = (a.K + b - 1) / b;
-    a.tc = (a.C + b - 1) / b;
-    const int64_t slots = int64_t(a.s.chunks) * a.s.per;
-    const int slices = int((slots + bk - 1) / bk), blocks = a.tr * a.tc;
-    const int want = std::max(1, std::min(512 / std::max(1, blocks), (slices + 3) / 4));
+template <typename S>
+static void plan(LinWgradArgs& a) {
+    a.tr = (a.K + S::BM - 1) / S::BM;
+    a.tc = (a.C + S::BN - 1) / S::BN;
+    const int slices = int((int64_t(a.s.chunks) * a.s.per + S::BK - 1) / S::BK), blocks = a.tr * a.tc, least = 4 * 128 / S::ROWB;
+    const int want = std::max(1, std::min(512 / std::max(1, blocks), (slices + least - 1) / least));
     a.per = (slices + want - 1) / want;
     a.shares = (slices + a.per - 1) / a.per;
+}
+
+void linear_wgrad_plan(LinWgradArgs& a, bool f32) {
+    if (big(a)) f32 ? plan<Big<float>>(a) : plan<Big<__bf16>>(a);
+    else f32 ? plan<Small<float>>(a) : plan<Small<__bf16>>(a);
 }
 
 size_t linear_wgrad_part_bytes(const LinWgradArgs& a) {
     return a.shares == 1 ? 0 : (size_t(a.shares) * a.K * (size_t(a.C) + 1) * sizeof(float) + 15) / 16 * 16;
 }
 
-template <typename T>
+template <typename S>
 static void launch(const LinWgradArgs& a, hipStream_t s) {
-    const dim3 g(unsigned(a.tr) * a.tc * a.shares), t(kLinThreads);
-    const bool big = block_of(a) == 128;
-    if (a.cl && big) hipLaunchKernelGGL((linear_wgrad_kernel<T, true, 128, 128>), g, t, 0, s, a);
-    else if (a.cl) hipLaunchKernelGGL((linear_wgrad_kernel<T, true, 64, 64>), g, t, 0, s, a);
-    else if (big) hipLaunchKernelGGL((linear_wgrad_kernel<T, false, 128, 128>), g, t, 0, s, a);
-    else hipLaunchKernelGGL((linear_wgrad_kernel<T, false, 64, 64>), g, t, 0, s, a);
+    const dim3 g(unsigned(a.tr) * a.tc * a.shares), t(S::TH);
+    if (a.cl && a.direct) hipLaunchKernelGGL((linear_wgrad_kernel<S, true, true>), g, t, 0, s, a);
+    else if (a.cl) hipLaunchKernelGGL((linear_wgrad_kernel<S, true, false>), g, t, 0, s, a);
+    else if (a.direct) hipLaunchKernelGGL((linear_wgrad_kernel<S, false, true>), g, t, 0, s, a);
+    else hipLaunchKernelGGL((linear_wgrad_kernel<S, false, false>), g, t, 0, s, a);
 }
 
 hipError_t launch_linear_wgrad(const LinWgradArgs& a, bool f32, hipStream_t s) {
-    if (f32) launch<float>(a, s);
-    else launch<__bf16>(a, s);
+    if (big(a)) f32 ? launch<Big<float>>(a, s) : launch<Big<__bf16>>(a, s);
+    else f32 ? launch<Small<float>>(a, s) : launch<Small<__bf16>>(a, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.shares == 1) return e;
     const int64_t all = int64_t(a.K) * a.C + (a.db ? a.K : 0);
-    hipLaunchKernelGGL(linear_wgrad_sum_kernel, dim3(unsigned((all + 255) / 256)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(linear_wgrad_sum_kernel, dim3(unsigned((all + 63) / 64)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
