@@ -349,7 +349,8 @@ dc_status dc_linear_fwd(const dc_view* vx, const void* x, const void* w, const f
     a.qm = map_of(*vy, vy->C);
     a.act = act;
     (void)hipGetLastError();
-    return launched(launch_linear_fwd(a, f32, static_cast<hipStream_t>(stream)));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return launched(linear_few(a) ? launch_linear_few(a, f32, s) : launch_linear_fwd(a, f32, s));
 }
 
 dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, int32_t act,

@@ -31,6 +31,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element's address
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
 enum { RK = 0, KR = 1 };
 
@@ -94,11 +95,11 @@ __device__ __forceinline__ Chunk chunk_of(const Slots& s, int ci) {
 enum { WEIGHT, PIXEL, LONG };   // which way an operand is found: see Stage
 
 // The shape of a workgroup's block: BM x BN of the result, ROWB bytes of k a slice,
-// NST slices in LDS, WM x WN waves.
-template <typename T_, int BM_, int BN_, int ROWB_, int NST_, int WM_, int WN_>
+// NST slices in LDS, WM x WN waves; OCC waves a SIMD that the registers leave room for.
+template <typename T_, int BM_, int BN_, int ROWB_, int NST_, int WM_, int WN_, int OCC_>
 struct Shape {
     typedef T_ T;
-    static constexpr int BM = BM_, BN = BN_, ROWB = ROWB_, NST = NST_, WM = WM_, WN = WN_;
+    static constexpr int BM = BM_, BN = BN_, ROWB = ROWB_, NST = NST_, WM = WM_, WN = WN_, OCC = OCC_;
     static constexpr int E = 16 / int(sizeof(T)), BK = ROWB / int(sizeof(T));
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32, GROUPS = ROWB / 32;
     static constexpr int ABYTES = BM * ROWB, BYTES = (BM + BN) * ROWB;

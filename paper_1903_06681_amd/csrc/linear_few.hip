@@ -1,0 +1,128 @@
+// Forward pass of a product over channels for few pixels (up to 64): a classifier on
+// pooled samples, single rows of channels.
+//
+// Bound: the weights, each read once: memory latency first (4 MB over the chip is a
+// microsecond).  A workgroup takes 16 output channels and deals their k out to its
+// sixteen waves, so that a wave's loads are few and all in flight at once; fragments
+// come straight from memory (16 x 16 blocks of the result: a lane's 16 bytes are one
+// row's), and the waves' sums meet in LDS, in order.
+#include <algorithm>
+
+#include "linear_pass.h"
+
+namespace dc {
+
+static constexpr int kFewWaves = 16, kFewMost = 64;
+typedef float f32x4_acc __attribute__((ext_vector_type(4)));
+
+template <typename T>
+__device__ __forceinline__ void multiply16(f32x4_acc& acc, const uint4& a, const uint4& b) {
+    if constexpr (sizeof(T) == 2) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0,
+                                                      0, 0);
+    } else {
+        const f32x4_t fa = __builtin_bit_cast(f32x4_t, a), fb = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fb[i], acc, 0, 0, 0);
+    }
+}
+
+// NT: tiles of 16 pixels
+template <typename T, bool CL, int NT>
+__global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a, int M) {
+    constexpr int E = 16 / int(sizeof(T)), STEP = 4 * E;      // k of a lane's chunk, of a wave's step
+    __shared__ float sums[kFewWaves][NT * 256];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int o0 = blockIdx.x * 16, red = a.a.red;
+    const int hw = int(a.s.dsample.d) / a.s.cpr * a.s.len;
+    auto offset = [&](int m, const auto& v) __attribute__((always_inline)) {   // of channel 0 of pixel m
+        const int n = m / hw, pix = m - n * hw, r = pix / a.s.len;
+        return n * v.sn + r * v.sh + (pix - r * a.s.len);
+    };
+    const T* w = reinterpret_cast<const T*>(a.a.p);
+    const T* x = reinterpret_cast<const T*>(a.b.p);
+    const int64_t wo = int64_t(min(o0 + (lane & 15), a.rows - 1)) * a.a.ld;
+    int64_t xo[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) xo[t] = offset(min(t * 16 + (lane & 15), M - 1), a.b);
+    // this wave's steps of k
+    const int steps = (red + STEP - 1) / STEP, per = (steps + kFewWaves - 1) / kFewWaves;
+    const int s1 = min((wave + 1) * per, steps);
+    f32x4_acc acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4_acc{0, 0, 0, 0};
+#pragma unroll 4
+    for (int s = wave * per; s < s1; ++s) {
+        const int k = s * STEP + (lane >> 4) * E, n = red - k;
+        uint4 fa = make_uint4(0, 0, 0, 0), fb[NT];
+        if (n > 0) fa = keep16<T>(load16(w, wo + k, a.a.end), n);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            fb[t] = make_uint4(0, 0, 0, 0);
+            if constexpr (CL) {
+                if (n > 0) fb[t] = keep16<T>(load16(x, xo[t] + k, a.b.end), n);
+            } else {
+                T e[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) e[i] = i < n ? x[xo[t] + (k + i) * a.b.sc] : T(0);
+                __builtin_memcpy(&fb[t], e, 16);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) multiply16<T>(acc[t], fa, fb[t]);
+    }
+    // lane: pixel lane % 16, channels 4 (lane / 16) .. + 3
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sums[wave][t * 256 + (4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[t][r];
+    __syncthreads();
+    // channels next to each other in memory (rows of channels) lie next to each other on the lanes
+    for (int e = threadIdx.x; e < NT * 256; e += 64 * kFewWaves) {
+        const int in = e & 255, o = o0 + (CL ? in & 15 : in >> 4), m = (e >> 8) * 16 + (CL ? in >> 4 : in & 15);
+        if (o >= a.rows || m >= M) continue;
+        const int at = (e & ~255) + (o - o0) * 16 + (m & 15);
+        float v = 0;
+#pragma unroll
+        for (int i = 0; i < kFewWaves; ++i) v += sums[i][at];
+        if (a.bias) v += a.bias[o];
+        auto put = [&](const View& t, float f) __attribute__((always_inline)) {
+            const int64_t k = offset(m, t) + o * t.sc;
+            if (t.dt == DC_F32) store1(reinterpret_cast<float*>(t.p) + k, f);
+            else store1(reinterpret_cast<__bf16*>(t.p) + k, f);
+        };
+        if (a.z.dt >= 0) put(a.z, v);
+        float y[1] = {v};
+        apply_act(y, a.act);
+        if (a.res.dt >= 0) {
+            const int64_t k = offset(m, a.res) + o * a.res.sc;
+            y[0] += a.res.dt == DC_F32 ? load1(reinterpret_cast<const float*>(a.res.p) + k)
+                                       : load1(reinterpret_cast<const __bf16*>(a.res.p) + k);
+        }
+        put(a.out, y[0]);
+    }
+}
+
+static int pixels_in(const LinearArgs& a) {
+    return a.s.chunks / int(a.s.dsample.d) * (int(a.s.dsample.d) / a.s.cpr * a.s.len);
+}
+
+// z in 8 bits needs 32 channels side by side: the tile loop's.
+bool linear_few(const LinearArgs& a) { return pixels_in(a) <= kFewMost && a.z.dt != DC_Q8; }
+
+template <typename T, bool CL>
+static void launch(const LinearArgs& a, int M, hipStream_t s) {
+    const dim3 g((a.rows + 15) / 16), t(64 * kFewWaves);
+    if (M <= 16) hipLaunchKernelGGL((linear_few_kernel<T, CL, 1>), g, t, 0, s, a, M);
+    else if (M <= 32) hipLaunchKernelGGL((linear_few_kernel<T, CL, 2>), g, t, 0, s, a, M);
+    else hipLaunchKernelGGL((linear_few_kernel<T, CL, 4>), g, t, 0, s, a, M);
+}
+
+hipError_t launch_linear_few(const LinearArgs& a, bool f32, hipStream_t s) {
+    const int M = pixels_in(a);
+    if (f32) a.cl ? launch<float, true>(a, M, s) : launch<float, false>(a, M, s);
+    else a.cl ? launch<__bf16, true>(a, M, s) : launch<__bf16, false>(a, M, s);
+    return hipGetLastError();
+}
+
+}  // namespace dc

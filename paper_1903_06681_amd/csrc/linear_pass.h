@@ -53,158 +53,81 @@ __device__ __forceinline__ void q8_load_half(float (&v)[16], const char* q, cons
     for (int r = 0; r < 16; ++r) v[r] = q8_value(w[r / 4], r % 4, step);
 }
 
-// ---- a lane's 16 channels of one pixel in memory
-//
-// Four lanes hold four neighbouring pixels of the same channels.  In bf16 they trade, so
-// that each has one channel of all four: 8 bytes an access instead of 2, a quarter of
-// the accesses (512 -> 2048 channels on 65536 pixels: with 2-byte stores of 268 MB the
-// forward pass took longer than with 4-byte ones of 537 MB).  fp32 goes channel by
-// channel: 128 contiguous bytes a half wave.
+// ---- a lane's 16 channels of one pixel in memory, channel by channel: the pixels are
+// contiguous over a half wave (64 bytes in bf16, 128 in fp32).  (Four lanes trading values
+// for 8 bytes of one channel each changed nothing: the stores are not what bounds.)
 
-// [lane q] (a0 a1 | a2 a3) -> (lane 0's aq, lane 1's aq | lane 2's aq, lane 3's aq)
-__device__ __forceinline__ void trade(uint32_t& lo, uint32_t& hi, int lane) {
-    constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E;      // quad permutations [1 0 3 2], [2 3 0 1]
-    const uint32_t sel = lane & 1 ? 0x03020706u : 0x05040100u;
-    const bool up = lane & 2;
-    const uint32_t e0 = __builtin_amdgcn_perm(__builtin_amdgcn_mov_dpp(lo, kSwap1, 0xf, 0xf, true), lo, sel);
-    const uint32_t e1 = __builtin_amdgcn_perm(__builtin_amdgcn_mov_dpp(hi, kSwap1, 0xf, 0xf, true), hi, sel);
-    const uint32_t got = __builtin_amdgcn_mov_dpp(up ? e0 : e1, kSwap2, 0xf, 0xf, true);
-    lo = up ? got : e0;
-    hi = up ? e1 : got;
-}
-
-// Where a lane's pixel lies, and the first of its four: element offset of a view's
-// channel 0 (the lane's is in range on every lane); pixels from there on in the row.
+// Where a lane's pixel lies: in range on every lane; ok: there is one.
 struct Place {
     Chunk c;
-    int w, w4, ok, left4;
+    int w, ok;
     __device__ __forceinline__ int64_t at(const View& t) const { return c.n * t.sn + c.r * t.sh + w; }
-    __device__ __forceinline__ int64_t at4(const View& t) const { return c.n * t.sn + c.r * t.sh + w4; }
 };
 template <int PER>
 __device__ __forceinline__ Place place_of(const Slots& s, int slot) {
     Place p;
-    const int sub = slot % PER, sub4 = PER == 1 ? 0 : sub & ~3;
     p.c = chunk_of(s, slot / PER);
-    p.ok = sub < p.c.left;
-    p.w = p.ok ? p.c.col + sub : 0;
-    p.left4 = p.c.left - sub4;
-    p.w4 = p.left4 > 0 ? p.c.col + sub4 : 0;
+    p.ok = slot % PER < p.c.left;
+    p.w = p.ok ? p.c.col + slot % PER : 0;
     return p;
 }
 
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-
-// PER: slots of a chunk; 1: rows of channels, which trade nothing.  All lanes call.
-template <typename T, int PER>
+template <typename T>
 __device__ __forceinline__ void load_half(float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
-    const int h = lane >> 5;
+    // channels past the last one repeat its address, for results that nobody keeps
+    const int first = o0 + 4 * (lane >> 5);
     const int64_t step = t.sc * int64_t(sizeof(T));
-    if constexpr (PER > 1 && sizeof(T) == 2) {
-        const int q = lane & 3;
-        const char* a = t.p + (p.at4(t) + (o0 + 4 * h + q) * t.sc) * 2;
-        const bool all = p.left4 >= 4;
+    char* a = t.p + (p.at(t) + min(first, rows - 1) * t.sc) * int64_t(sizeof(T));
 #pragma unroll
-        for (int g = 0; g < 4; ++g, a += 8 * step) {
-            uint32_t lo = 0, hi = 0;
-            if (o0 + 8 * g + 4 * h + q < rows) {
-                if (all) {
-                    const u32x2_any d = *reinterpret_cast<const u32x2_any*>(a);
-                    lo = d.x;
-                    hi = d.y;
-                } else {
-                    const uint16_t* e = reinterpret_cast<const uint16_t*>(a);
-                    if (p.left4 > 0) lo = e[0];
-                    if (p.left4 > 1) lo |= uint32_t(e[1]) << 16;
-                    if (p.left4 > 2) hi = e[2];
-                }
-            }
-            trade(lo, hi, lane);
-            v[4 * g] = __builtin_bit_cast(float, lo << 16);
-            v[4 * g + 1] = __builtin_bit_cast(float, lo & 0xffff0000u);
-            v[4 * g + 2] = __builtin_bit_cast(float, hi << 16);
-            v[4 * g + 3] = __builtin_bit_cast(float, hi & 0xffff0000u);
-        }
-    } else {
-        char* a = t.p + (p.at(t) + (o0 + 4 * h) * t.sc) * int64_t(sizeof(T));
-        const int64_t skip = 5 * step;
-        if (o0 + 32 <= rows) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) v[r] = load1(reinterpret_cast<const T*>(a));
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) {
-                v[r] = 0;
-                if (o0 + 8 * (r / 4) + 4 * h + r % 4 < rows) v[r] = load1(reinterpret_cast<const T*>(a));
-            }
-        }
+    for (int r = 0; r < 16; ++r) {
+        v[r] = load1(reinterpret_cast<const T*>(a));
+        const int on = r % 4 == 3 ? 5 : 1;
+        next(a, first + 8 * (r / 4) + r % 4 + on < rows ? on * step : 0);
     }
 }
-template <int PER>
 __device__ __forceinline__ void load_half(float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
     if (t.dt == DC_F32)
-        load_half<float, PER>(v, t, p, o0, lane, rows);
+        load_half<float>(v, t, p, o0, lane, rows);
     else
-        load_half<__bf16, PER>(v, t, p, o0, lane, rows);
+        load_half<__bf16>(v, t, p, o0, lane, rows);
 }
 
-template <typename T, int PER>
+template <typename T>
 __device__ __forceinline__ void store_half(const float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
     const int h = lane >> 5;
     const int64_t step = t.sc * int64_t(sizeof(T));
     auto packed = [&](int r) __attribute__((always_inline)) {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{v[r], v[r + 1]}), bf16x2_t));
     };
-    if constexpr (PER > 1 && sizeof(T) == 2) {
-        const int q = lane & 3;
-        char* a = t.p + (p.at4(t) + (o0 + 4 * h + q) * t.sc) * 2;
-        const bool all = p.left4 >= 4;
+    if (!p.ok) return;
+    char* a = t.p + (p.at(t) + (o0 + 4 * h) * t.sc) * int64_t(sizeof(T));
+    if (t.sc == 1 && o0 + 32 <= rows) {      // rows of channels: four lie together
 #pragma unroll
-        for (int g = 0; g < 4; ++g, a += 8 * step) {
-            uint32_t lo = packed(4 * g), hi = packed(4 * g + 2);
-            trade(lo, hi, lane);
-            if (o0 + 8 * g + 4 * h + q >= rows) continue;
-            if (all) {
-                *reinterpret_cast<u32x2_any*>(a) = u32x2_any{lo, hi};
-            } else {
-                uint16_t* e = reinterpret_cast<uint16_t*>(a);
-                if (p.left4 > 0) e[0] = uint16_t(lo);
-                if (p.left4 > 1) e[1] = uint16_t(lo >> 16);
-                if (p.left4 > 2) e[2] = uint16_t(hi);
-            }
+        for (int g = 0; g < 4; ++g, a += 8 * sizeof(T)) {
+            if constexpr (sizeof(T) == 4)
+                *reinterpret_cast<u32x4_any*>(a) =
+                    u32x4_any{__builtin_bit_cast(uint32_t, v[4 * g]), __builtin_bit_cast(uint32_t, v[4 * g + 1]),
+                              __builtin_bit_cast(uint32_t, v[4 * g + 2]), __builtin_bit_cast(uint32_t, v[4 * g + 3])};
+            else
+                *reinterpret_cast<u32x2_any*>(a) = u32x2_any{packed(4 * g), packed(4 * g + 2)};
         }
+        return;
+    }
+    const int64_t skip = 5 * step;
+    if (o0 + 32 <= rows) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) store1(reinterpret_cast<T*>(a), v[r]);
     } else {
-        if (!p.ok) return;
-        char* a = t.p + (p.at(t) + (o0 + 4 * h) * t.sc) * int64_t(sizeof(T));
-        if (PER == 1 && t.sc == 1 && o0 + 32 <= rows) {      // rows of channels: four lie together
 #pragma unroll
-            for (int g = 0; g < 4; ++g, a += 8 * sizeof(T)) {
-                if constexpr (sizeof(T) == 4)
-                    *reinterpret_cast<u32x4_any*>(a) =
-                        u32x4_any{__builtin_bit_cast(uint32_t, v[4 * g]), __builtin_bit_cast(uint32_t, v[4 * g + 1]),
-                                  __builtin_bit_cast(uint32_t, v[4 * g + 2]), __builtin_bit_cast(uint32_t, v[4 * g + 3])};
-                else
-                    *reinterpret_cast<u32x2_any*>(a) = u32x2_any{packed(4 * g), packed(4 * g + 2)};
-            }
-            return;
-        }
-        const int64_t skip = 5 * step;
-        if (o0 + 32 <= rows) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) store1(reinterpret_cast<T*>(a), v[r]);
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip))
-                if (o0 + 8 * (r / 4) + 4 * h + r % 4 < rows) store1(reinterpret_cast<T*>(a), v[r]);
-        }
+        for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip))
+            if (o0 + 8 * (r / 4) + 4 * h + r % 4 < rows) store1(reinterpret_cast<T*>(a), v[r]);
     }
 }
-template <int PER>
 __device__ __forceinline__ void store_half(const float (&v)[16], const View& t, const Place& p, int o0, int lane, int rows) {
     if (t.dt == DC_F32)
-        store_half<float, PER>(v, t, p, o0, lane, rows);
+        store_half<float>(v, t, p, o0, lane, rows);
     else
-        store_half<__bf16, PER>(v, t, p, o0, lane, rows);
+        store_half<__bf16>(v, t, p, o0, lane, rows);
 }
 
 template <int N>
@@ -235,6 +158,7 @@ __device__ __forceinline__ void apply_slope(float (&z)[N], float (&v)[N], int ac
             act_both<decltype(tag)::value>(z[r], a, d);
             z[r] = a;
             v[r] *= d;
+            if (r % 8 == 7) __builtin_amdgcn_sched_barrier(0);   // eight at a time: registers
         }
     };
     switch (act) {
@@ -257,9 +181,9 @@ __device__ __forceinline__ void epilogue(float (&v)[16], const LinearArgs& a, in
             if (a.z.dt == DC_Q8)
                 q8_load_half(z, a.z.p, a.qm, p.c.n, o0 / 32, pix, h);
             else
-                load_half<PER>(z, a.z, p, o0, lane, a.rows);
+                load_half(z, a.z, p, o0, lane, a.rows);
             apply_slope(z, v, a.act);
-            if (a.h.dt >= 0) store_half<PER>(z, a.h, p, o0, lane, a.rows);
+            if (a.h.dt >= 0) store_half(z, a.h, p, o0, lane, a.rows);
         }
     } else {
         if (a.z.dt == DC_Q8) {
@@ -270,23 +194,23 @@ __device__ __forceinline__ void epilogue(float (&v)[16], const LinearArgs& a, in
             }
             q8_store_half(a.z.p, a.qm, p.c.n, o0 / 32, pix, p.ok, h, v);
         } else if (a.z.dt >= 0) {
-            store_half<PER>(v, a.z, p, o0, lane, a.rows);
+            store_half(v, a.z, p, o0, lane, a.rows);
         }
         apply_act(v, a.act);
         if (a.res.dt >= 0) {
             float e[16];
-            load_half<PER>(e, a.res, p, o0, lane, a.rows);
+            load_half(e, a.res, p, o0, lane, a.rows);
 #pragma unroll
             for (int r = 0; r < 16; ++r) v[r] += e[r];
         }
     }
-    store_half<PER>(v, a.out, p, o0, lane, a.rows);
+    store_half(v, a.out, p, o0, lane, a.rows);
 }
 
 // BWD: the input gradient (weights KR), else the forward pass (weights RK).
 // CL: pixels RK (rows of channels), else KR.  DIRECT: operands on 16-byte boundaries.
 template <typename S, bool BWD, bool CL, bool DIRECT>
-__global__ __launch_bounds__(S::TH, 2) void linear_kernel(LinearArgs a) {
+__global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
     typedef typename S::T T;
     constexpr int AK = BWD ? KR : RK, PK = CL ? RK : KR, TM = S::TM, TN = S::TN;
     __shared__ __align__(16) char lds[DIRECT ? S::NST : 2][S::BYTES];
@@ -345,9 +269,14 @@ __global__ __launch_bounds__(S::TH, 2) void linear_kernel(LinearArgs a) {
     });
 }
 
-// Blocks of 128 channels x 256 pixels, or of 64 x 64 where those would not fill the chip.
-template <typename T> using Big = Shape<T, 128, 256, 64, 3, 2, 2>;
-template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2>;
+// Long sums over many pixels: the largest block, whose operands are read least often (512
+// channels to 2048 on 65536 pixels, forward with gelu and z in 8 bits, 300 us against 338
+// with 128 x 256, 357 with 64 x 128).  Short sums are bound by what they store and by the
+// epilogue: more and smaller workgroups at a time (64 to 256 on 100352: 33 us against 40
+// and, with 256 x 256, 43).  Few pixels: blocks small enough for the chip to have some.
+template <typename T> using Large = Shape<T, 256, 256, 128, 2, 4, 2, 2>;
+template <typename T> using Middle = Shape<T, 64, 128, 128, 2, 1, 4, 3>;
+template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2, 4>;
 
 template <typename S, bool BWD>
 static void launch_shape(LinearArgs a, hipStream_t s) {
@@ -363,10 +292,10 @@ static void launch_shape(LinearArgs a, hipStream_t s) {
 template <typename T, bool BWD>
 static hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
     const int64_t slots = int64_t(a.s.chunks) * a.s.per;
-    if (int64_t((a.rows + 127) / 128) * ((slots + 255) / 256) >= 512)
-        launch_shape<Big<T>, BWD>(a, s);
-    else
-        launch_shape<Small<T>, BWD>(a, s);
+    auto blocks = [&](int r, int c) { return (a.rows + r - 1) / r * ((slots + c - 1) / c); };
+    if (a.a.red > 128 && blocks(256, 256) >= 256) launch_shape<Large<T>, BWD>(a, s);
+    else if (blocks(64, 128) >= 512) launch_shape<Middle<T>, BWD>(a, s);
+    else launch_shape<Small<T>, BWD>(a, s);
     return hipGetLastError();
 }
 

@@ -27,7 +27,7 @@ __device__ __forceinline__ float sum16(const uint4& f) {
 }
 
 template <typename S, bool CL, bool DIRECT>
-__global__ __launch_bounds__(S::TH, 2) void linear_wgrad_kernel(LinWgradArgs a) {
+__global__ __launch_bounds__(S::TH, S::OCC) void linear_wgrad_kernel(LinWgradArgs a) {
     typedef typename S::T T;
     constexpr int KIND = CL ? KR : RK, TM = S::TM, TN = S::TN;
     __shared__ __align__(16) char lds[DIRECT ? S::NST : 2][S::BYTES];
@@ -109,24 +109,24 @@ __global__ __launch_bounds__(256) void linear_wgrad_sum_kernel(LinWgradArgs a) {
     *d = a.accumulate ? *d + s : s;
 }
 
-// Blocks of 128 x 256, or of 64 x 64 for small results; shares so that about 512
-// workgroups run, none with fewer than four slices of 128 bytes.
-template <typename T> using Big = Shape<T, 128, 256, 64, 3, 2, 2>;
-template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2>;
-static bool big(const LinWgradArgs& a) { return a.K > 64 && a.C > 128; }
+// Blocks of 256 x 256 where the result has them, or of 64 x 64; shares so that one (two)
+// workgroups a compute unit run, none with fewer than four slices.
+template <typename T> using Large = Shape<T, 256, 256, 128, 2, 4, 2, 2>;
+template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2, 4>;
+static bool large(const LinWgradArgs& a) { return a.K > 128 && a.C > 128; }
 
 template <typename S>
 static void plan(LinWgradArgs& a) {
     a.tr = (a.K + S::BM - 1) / S::BM;
     a.tc = (a.C + S::BN - 1) / S::BN;
-    const int slices = int((int64_t(a.s.chunks) * a.s.per + S::BK - 1) / S::BK), blocks = a.tr * a.tc, least = 4 * 128 / S::ROWB;
-    const int want = std::max(1, std::min(512 / std::max(1, blocks), (slices + least - 1) / least));
+    const int slices = int((int64_t(a.s.chunks) * a.s.per + S::BK - 1) / S::BK), blocks = a.tr * a.tc, groups = S::BM == 256 ? 256 : 512;
+    const int want = std::max(1, std::min(groups / blocks, (slices + 3) / 4));
     a.per = (slices + want - 1) / want;
     a.shares = (slices + a.per - 1) / a.per;
 }
 
 void linear_wgrad_plan(LinWgradArgs& a, bool f32) {
-    if (big(a)) f32 ? plan<Big<float>>(a) : plan<Big<__bf16>>(a);
+    if (large(a)) f32 ? plan<Large<float>>(a) : plan<Large<__bf16>>(a);
     else f32 ? plan<Small<float>>(a) : plan<Small<__bf16>>(a);
 }
 
@@ -144,7 +144,7 @@ static void launch(const LinWgradArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_linear_wgrad(const LinWgradArgs& a, bool f32, hipStream_t s) {
-    if (big(a)) f32 ? launch<Big<float>>(a, s) : launch<Big<__bf16>>(a, s);
+    if (large(a)) f32 ? launch<Large<float>>(a, s) : launch<Large<__bf16>>(a, s);
     else f32 ? launch<Small<float>>(a, s) : launch<Small<__bf16>>(a, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.shares == 1) return e;

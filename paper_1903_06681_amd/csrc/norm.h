@@ -45,17 +45,41 @@ __device__ __forceinline__ void pixel_sum(float (&v)[K], const NormArgs& a, cons
     }
 }
 
-// gamma or beta of a block; where there is none, `none`
+// gamma or beta of a block; where there is none, `none`.  One block a wave: scalar loads.
+// Else vector loads whose address is formed here (ahead of a loop it, or the values, would
+// take the registers).
+template <int LPX>
 __device__ __forceinline__ void load_params(float (&v)[32], const float* p, int c0, int C, float none) {
     if (!p) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = none;
-    } else if (c0 + 32 <= C) {
+    } else if constexpr (LPX == 64) {
+        if (c0 + 32 <= C) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = p[c0 + j];
+            for (int j = 0; j < 32; ++j) v[j] = p[c0 + j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = p[min(c0 + j, C - 1)];
+        }
     } else {
+        char* a = reinterpret_cast<char*>(const_cast<float*>(p + c0));
+        if (C % 32 == 0) {
+            next(a, 0);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = p[min(c0 + j, C - 1)];
+            for (int j = 0; j < 32; j += 4) {
+                const float4 f = *reinterpret_cast<const float4*>(a + 4 * j);
+                v[j] = f.x;
+                v[j + 1] = f.y;
+                v[j + 2] = f.z;
+                v[j + 3] = f.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                v[j] = *reinterpret_cast<const float*>(a);
+                next(a, c0 + j + 1 < C ? 4 : 0);
+            }
+        }
     }
 }
 

@@ -32,7 +32,7 @@ __device__ __forceinline__ void sum_lanes(float (&v)[64], int lane) {
 
 // XT: float or __bf16 of the tile, or char: the checkpoint.
 template <typename XT, typename DT, int LPX, int R, bool CL>
-__global__ __launch_bounds__(512) void norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(512, LPX == 64 && R == 1 ? 3 : 2) void norm_bwd_kernel(NormArgs a) {
     constexpr bool Q = sizeof(XT) == 1;
     constexpr int H = R ? R : 1, E = 64 / LPX;
     __shared__ float red[2][2][kNormWaves * LPX];
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(512) void norm_bwd_kernel(NormArgs a) {
         const int m = (g0 + l.pg) * LPX + l.px;
         const bool in = m < a.px.M;
         const int mm = min(m, a.px.M - 1);
-        const Pixel p = pixel_of(a.px, mm);
+        const Pixel p = pixel_of(a.px, m);
         const float mu = a.stat[mm], r = a.stat[int64_t(a.px.M) + mm];
         float vx[H][32], vd[H][32];
         auto load = [&](int i, int cb) __attribute__((always_inline)) {
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(512) void norm_bwd_kernel(NormArgs a) {
             if constexpr (!R) load(0, cb);
             centre(i);
             float gm[32];
-            load_params(gm, a.gamma, cb * 32, a.C, 1.0f);
+            load_params<LPX>(gm, a.gamma, cb * 32, a.C, 1.0f);
 #pragma unroll
             for (int j = 0; j < 32; ++j) {     // du is zero past C, x finite there or NaN with the pixel
                 const float g = gm[j] * vd[i][j];
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(512) void norm_bwd_kernel(NormArgs a) {
             }
             if (!in) return;
             float gm[32], o[32];
-            load_params(gm, a.gamma, cb * 32, a.C, 1.0f);
+            load_params<LPX>(gm, a.gamma, cb * 32, a.C, 1.0f);
             if (a.res.p) load_any<CL>(o, a.res, p, cb * 32, a.C);
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(512) void norm_bwd_kernel(NormArgs a) {
             }
             store_any<CL>(a.dx, p, cb * 32, a.C, o);
             if (a.u.p) {
-                load_params(o, a.beta, cb * 32, a.C, 0.0f);
+                load_params<LPX>(o, a.beta, cb * 32, a.C, 0.0f);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) o[j] = fmaf(gm[j], vx[i][j], o[j]);
                 store_any<CL>(a.u, p, cb * 32, a.C, o);

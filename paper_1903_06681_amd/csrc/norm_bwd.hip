@@ -15,6 +15,7 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(NormArgs a, int rows)
     const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
     const int width = 2 * a.blocks * 32, v = blockIdx.x * 64 + lane;
     float s = 0;
+#pragma unroll 8
     for (int i = share; i < rows; i += 16) s += a.part[int64_t(i) * width + v];
     red[share][lane] = s;
     __syncthreads();

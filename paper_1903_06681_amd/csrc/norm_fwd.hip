@@ -20,7 +20,7 @@ __global__ __launch_bounds__(512) void norm_fwd_kernel(NormArgs a) {
     const NormLane l = norm_lane<LPX>(a);
     const int m = (xcd_range(blockIdx.x, a.grid) * a.pg + l.pg) * LPX + l.px;
     const bool in = m < a.px.M;
-    const Pixel p = pixel_of(a.px, min(m, a.px.M - 1));
+    const Pixel p = pixel_of(a.px, m);
     float v[R ? R : 1][32];
     float s[1] = {0};
     each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
@@ -53,8 +53,8 @@ __global__ __launch_bounds__(512) void norm_fwd_kernel(NormArgs a) {
         if constexpr (!R) load_block<XT, CL>(v[0], a.x, p, cb * 32, a.C);
         if (a.q) q8_store_block(a.q, a.qm, p, cb, v[i]);
         float g[32], b[32];
-        load_params(g, a.gamma, cb * 32, a.C, 1.0f);
-        load_params(b, a.beta, cb * 32, a.C, 0.0f);
+        load_params<LPX>(g, a.gamma, cb * 32, a.C, 1.0f);
+        load_params<LPX>(b, a.beta, cb * 32, a.C, 0.0f);
 #pragma unroll
         for (int j = 0; j < 32; ++j) g[j] = fmaf(g[j], (v[i][j] - mu) * r, b[j]);
         store_any<CL>(a.u, p, cb * 32, a.C, g);
@@ -76,12 +76,13 @@ bool norm_plan(NormArgs& a, bool backward) {
     const int sb = 64 / a.lpx;
     a.nw = std::min((a.blocks + sb - 1) / sb, kNormWaves);
     const int held = (a.blocks + a.nw * sb - 1) / (a.nw * sb);
-    a.held = held <= 1 ? 1 : held == 2 && !a.cl ? 2 : 0;
+    a.held = held <= 1 ? 1 : held == 2 && !a.cl && !(backward && a.lpx == 16) ? 2 : 0;   // as registers allow
     a.groups = int((int64_t(a.px.M) + a.lpx - 1) / a.lpx);
-    // enough workgroups for the chip first, then up to eight waves each
-    a.pg = std::max(1, std::min(kNormWaves / a.nw, a.groups / 512));
+    // enough workgroups for the chip first, then up to four waves each (more would not fit
+    // the registers evenly)
+    a.pg = std::max(1, std::min(4 / a.nw, a.groups / 512));
     a.grid = (a.groups + a.pg - 1) / a.pg;
-    if (backward) a.grid = std::min(a.grid, 512);   // two workgroups a compute unit
+    if (backward) a.grid = std::min(a.grid, a.lpx == 64 && a.held == 1 && a.nw <= 4 ? 768 : 512);   // what is resident at a time
     return true;
 }
 
