@@ -200,15 +200,21 @@ __device__ __forceinline__ void load_block(float (&v)[32], const View& t, const 
 #pragma unroll
             for (int j = 0; j < 32; ++j, next(a, step)) v[j] = load1(reinterpret_cast<const T*>(a));
         } else {
-            // Channels past C repeat the last one's address and count as zero: no branches
-            // (a branch a channel waits for each load in turn).
+            // Channels past C repeat the last one's address and count as zero: a branch for
+            // eight of them, not for each (which waits for each load in turn).
             int left = C - c0;
             asm volatile("" : "+v"(left));   // 32 comparisons here, not 32 results ahead of a loop
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const float f = load1(reinterpret_cast<const T*>(a));
-                v[j] = j < left ? f : 0.0f;
-                next(a, j + 1 < left ? step : 0);
+            for (int j = 0; j < 32; ++j) v[j] = 0;
+#pragma unroll
+            for (int g = 0; g < 32; g += 8) {
+                if (!__any(g < left)) break;
+#pragma unroll
+                for (int j = g; j < g + 8; ++j) {
+                    const float f = load1(reinterpret_cast<const T*>(a));
+                    v[j] = j < left ? f : 0.0f;
+                    next(a, j + 1 < left ? step : 0);
+                }
             }
         }
     }

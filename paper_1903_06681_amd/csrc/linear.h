@@ -274,12 +274,13 @@ __device__ __forceinline__ void multiply(f32x16_t& acc, const uint4& a, const ui
 // from one slice to the next: before a slice's last group every wave has read all of it
 // (one barrier a slice), so its buffer is free and the next one's is in place.  DIRECT:
 // slices come straight into LDS, NST of them at a time; else through registers, two.
+// NST = 1: there is only one slice.
 template <typename S, int AK, int BK_, bool DIRECT, typename SA, typename SB, typename F>
 __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const SA& sa, const SB& sb, const Operand& oa,
                                           const Operand& ob, const Slots& s, int k0, int k1, char (*lds)[S::BYTES], int row0,
                                           int col0, int lane, F&& seen) {
     typedef typename S::T T;
-    constexpr int NST = DIRECT ? S::NST : 2, LOADS = SA::U + SB::U;
+    constexpr int NST = DIRECT || S::NST == 1 ? S::NST : 2, LOADS = SA::U + SB::U;
     uint4 fa[2][S::TM], fb[2][S::TN];
     auto read = [&](int to, const char* a, int g) __attribute__((always_inline)) {
 #pragma unroll
@@ -330,7 +331,7 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
 
     if constexpr (DIRECT) {
 #pragma unroll
-        for (int i = 0; i < NST - 1; ++i)
+        for (int i = 0; i < (NST > 1 ? NST - 1 : 1); ++i)
             if (i < n) fetch(i, i);
         arrived(0);
     } else {
@@ -339,13 +340,13 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
         if (1 < n) load(1);
     }
     __syncthreads();
-    if (DIRECT && NST - 1 < n) fetch(NST - 1, NST - 1);
+    if (DIRECT && NST > 1 && NST - 1 < n) fetch(NST - 1, NST - 1);
     read(0, lds[0], 0);
     int buf = 0;
     for (int step = 0; step < n; ++step) {
         const int next = buf + 1 == NST ? 0 : buf + 1;
         const bool more = step + 1 < n;
-        if (!DIRECT && more) {
+        if (!DIRECT && NST > 1 && more) {
             store(next);
             if (step + 2 < n) load(step + 2);
         }
@@ -353,7 +354,7 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
             constexpr int g = decltype(gc)::value;
             if constexpr (g + 1 < S::GROUPS) {
                 read((g + 1) & 1, lds[buf], g + 1);
-            } else if (more) {
+            } else if (NST > 1 && more) {
                 if (DIRECT) arrived(step + 1);
                 __syncthreads();
                 if (DIRECT && step + NST < n) fetch(step + NST, buf);

@@ -213,7 +213,8 @@ template <typename S, bool BWD, bool CL, bool DIRECT>
 __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
     typedef typename S::T T;
     constexpr int AK = BWD ? KR : RK, PK = CL ? RK : KR, TM = S::TM, TN = S::TN;
-    __shared__ __align__(16) char lds[DIRECT ? S::NST : 2][S::BYTES];
+    constexpr int NST = DIRECT || S::NST == 1 ? S::NST : 2;
+    __shared__ __align__(16) char lds[NST][S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // blocks of one column range follow each other on an XCD: they read the same pixels
     const int id = xcd_range(blockIdx.x, a.tr * a.tc);
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
     // The blocks of 32 x 32 pass through the wave's share of LDS, a lane's values back to
     // the lane: a loop at run time instead of one copy of the epilogue per block, which
     // overran the registers and the instruction cache.
-    constexpr int Q = TM * TN, ROOM = (DIRECT ? S::NST : 2) * S::BYTES / (S::TH * 64), PER = Q < ROOM ? Q : ROOM;
+    constexpr int Q = TM * TN, ROOM = NST * S::BYTES / (S::TH * 64), PER = Q < ROOM ? Q : ROOM;
     char* mine = &lds[0][0] + wave * (PER * 4096) + lane * 16;
     __syncthreads();
     static_for<0, (Q + PER - 1) / PER>([&](auto part) __attribute__((always_inline)) {
@@ -276,6 +277,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
 // and, with 256 x 256, 43).  Few pixels: blocks small enough for the chip to have some.
 template <typename T> using Large = Shape<T, 256, 256, 128, 2, 4, 2, 2>;
 template <typename T> using Middle = Shape<T, 64, 128, 128, 2, 1, 4, 3>;
+template <typename T> using Short = Shape<T, 64, 128, 128, 1, 1, 4, 4>;     // one slice: half the LDS
 template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2, 4>;
 
 template <typename S, bool BWD>
@@ -294,6 +296,7 @@ static hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
     const int64_t slots = int64_t(a.s.chunks) * a.s.per;
     auto blocks = [&](int r, int c) { return (a.rows + r - 1) / r * ((slots + c - 1) / c); };
     if (a.a.red > 128 && blocks(256, 256) >= 256) launch_shape<Large<T>, BWD>(a, s);
+    else if (blocks(64, 128) >= 512 && a.a.red <= Short<T>::BK) launch_shape<Short<T>, BWD>(a, s);
     else if (blocks(64, 128) >= 512) launch_shape<Middle<T>, BWD>(a, s);
     else launch_shape<Small<T>, BWD>(a, s);
     return hipGetLastError();
