@@ -14,7 +14,7 @@ namespace dc {
 
 static const int64_t kMaxPixels = (int64_t(1) << 31) - (int64_t(1) << 16);   // a block past the end still counts in 32 bits
 static const int32_t kMaxChannels = 1 << 20;
-static const int64_t kMaxBlocks = int64_t(1) << 23;
+static const int64_t kMaxBlocks = int64_t(1) << 22;   // of 128 x 128; threads are counted in 32 bits
 
 static bool misaligned(const void* p, size_t to = 16) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 static dc_status launched(hipError_t e) { return e == hipSuccess ? DC_OK : DC_ERR_HIP; }

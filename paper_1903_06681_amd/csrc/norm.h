@@ -115,7 +115,8 @@ __device__ __forceinline__ void each_block(const NormArgs& a, const NormLane& l,
 // Launch K<type, LPX, R, CL> as planned (norm_plan keeps to these).
 #define DC_NORM_LAUNCH(KERNEL, a, s, ...)                                                                       \
     do {                                                                                                        \
-        const dim3 g_((a).grid), b_(64 * (a).nw * (a).pg);                                                      \
+        const unsigned x_ = (a).grid < (1 << 22) ? (a).grid : 1 << 22;  /* threads of a dimension: 32 bits */   \
+        const dim3 g_(x_, ((a).grid + x_ - 1) / x_), b_(64 * (a).nw * (a).pg);                                  \
         if ((a).lpx == 64 && (a).held == 1) hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 64, 1, false>), g_, b_, 0, s, a);      \
         else if ((a).lpx == 64) hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 64, 2, false>), g_, b_, 0, s, a);       \
         else if ((a).lpx == 16 && !(a).cl && (a).held == 1)                                                     \

@@ -18,7 +18,10 @@ template <typename XT, int LPX, int R, bool CL>
 __global__ __launch_bounds__(512) void norm_fwd_kernel(NormArgs a) {
     __shared__ float red[2][1][kNormWaves * LPX];
     const NormLane l = norm_lane<LPX>(a);
-    const int m = (xcd_range(blockIdx.x, a.grid) * a.pg + l.pg) * LPX + l.px;
+    // workgroups past what one dimension of a grid counts lie in the second
+    const int wg = int(blockIdx.y * gridDim.x + blockIdx.x);
+    if (wg >= a.grid) return;
+    const int m = (xcd_range(wg, a.grid) * a.pg + l.pg) * LPX + l.px;
     const bool in = m < a.px.M;
     const Pixel p = pixel_of(a.px, m);
     float v[R ? R : 1][32];
