@@ -170,12 +170,13 @@ __device__ __forceinline__ void next(char*& p, int64_t step) {
     asm("" : "+v"(p));
 }
 
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element's address
+
 // Values of one pixel's block of 32 channels (first: c0), loaded and stored.  CL: the
-// channels are contiguous and lie on 16-byte boundaries (host check: C, the
-// strides and the base), so a block is whole 16-byte vectors; else every channel is an
-// access of its own, contiguous over the wave's pixels.  (In bf16 that is 2 bytes a lane.
-// Four lanes trading values for 8 bytes of one channel each were slower: a save of
-// 4 x 64 x 256 x 256 14.0 us against 10.2.)
+// channels are contiguous, so a block is 16-byte vectors (and single elements at C's end);
+// else every channel is an access of its own, contiguous over the wave's pixels.  (In bf16
+// that is 2 bytes a lane.  Four lanes trading values for 8 bytes of one channel each were
+// slower: a save of 4 x 64 x 256 x 256 14.0 us against 10.2.)
 template <typename T, bool CL>
 __device__ __forceinline__ void load_block(float (&v)[32], const View& t, const Pixel& p, int c0, int C) {
     char* a = spot_of<T>(t, p) + c0 * (CL ? 1 : t.sc) * int64_t(sizeof(T));
@@ -183,8 +184,16 @@ __device__ __forceinline__ void load_block(float (&v)[32], const View& t, const 
         constexpr int VE = 16 / int(sizeof(T));
 #pragma unroll
         for (int j = 0; j < 32 / VE; ++j) {
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (c0 + j * VE < C) u = *reinterpret_cast<const uint4*>(a + j * 16);
+            u32x4_any u{0, 0, 0, 0};
+            const int left = C - (c0 + j * VE);
+            if (left >= VE) {
+                u = *reinterpret_cast<const u32x4_any*>(a + j * 16);
+            } else if (left > 0) {
+                T e[VE];
+#pragma unroll
+                for (int i = 0; i < VE; ++i) e[i] = i < left ? reinterpret_cast<const T*>(a + j * 16)[i] : T(0);
+                __builtin_memcpy(&u, e, 16);
+            }
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
@@ -227,7 +236,13 @@ __device__ __forceinline__ void store_block(const View& t, const Pixel& p, int c
         constexpr int VE = 16 / int(sizeof(T));
 #pragma unroll
         for (int j = 0; j < 32 / VE; ++j) {
-            if (c0 + j * VE >= C) continue;
+            const int left = C - (c0 + j * VE);
+            if (left < VE) {
+#pragma unroll
+                for (int i = 0; i < VE; ++i)
+                    if (i < left) store1(reinterpret_cast<T*>(a + j * 16) + i, v[j * VE + i]);
+                continue;
+            }
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -237,7 +252,7 @@ __device__ __forceinline__ void store_block(const View& t, const Pixel& p, int c
                     w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
                                                             (f32x2_t{v[j * VE + 2 * i], v[j * VE + 2 * i + 1]}), bf16x2_t));
             }
-            *reinterpret_cast<uint4*>(a + j * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<u32x4_any*>(a + j * 16) = u32x4_any{w[0], w[1], w[2], w[3]};
         }
     } else {
         const int64_t step = t.sc * int64_t(sizeof(T));

@@ -86,14 +86,10 @@ struct Together {
             if (v[i]->H > 1 && v[i]->sh != v[i]->W) return false;
         return true;
     }
-    // rows of channels, every block of 8 channels on a 16-byte boundary
-    bool rows16() const {
-        for (int i = 0; i < n; ++i) {
-            const dc_view& a = *v[i];
-            const int e = 16 / esize(a);
-            if (a.W != 1 || a.sc != 1 || a.C % 8 || misaligned(p[i])) return false;
-            if ((a.N > 1 && a.sn % e) || (a.H > 1 && a.sh % e)) return false;
-        }
+    // rows of channels
+    bool rows() const {
+        for (int i = 0; i < n; ++i)
+            if (v[i]->W != 1 || v[i]->sc != 1) return false;
         return n > 0;
     }
 };
@@ -211,7 +207,7 @@ static dc_status ckpt_common(const dc_view* vx, const void* x, const void* q, in
     a.px = pixels_for(*vx, t.flat());
     a.C = vx->C;
     a.act = act;
-    a.cl = t.rows16();
+    a.cl = t.rows();
     (void)hipGetLastError();
     return launched(launch_ckpt(a, save, static_cast<hipStream_t>(stream)));
 }
@@ -252,7 +248,7 @@ dc_status dc_norm_fwd(const dc_view* vx, const void* x, const float* gamma, cons
     a.stat = stat;
     a.eps = eps;
     a.C = vx->C;
-    a.cl = t.rows16();
+    a.cl = t.rows();
     norm_plan(a, false);
     (void)hipGetLastError();
     return launched(launch_norm_fwd(a, static_cast<hipStream_t>(stream)));
@@ -305,7 +301,7 @@ dc_status dc_norm_bwd(const dc_view* vdu, const void* du, const dc_view* vx, con
     a.part = static_cast<float*>(workspace);
     a.C = vdu->C;
     a.accumulate = accumulate;
-    a.cl = t.rows16();
+    a.cl = t.rows();
     norm_plan(a, true);
     (void)hipGetLastError();
     return launched(launch_norm_bwd(a, static_cast<hipStream_t>(stream)));
@@ -350,7 +346,7 @@ dc_status dc_linear_fwd(const dc_view* vx, const void* x, const void* w, const f
     a.act = act;
     (void)hipGetLastError();
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return launched(linear_few(a) ? launch_linear_few(a, f32, s) : launch_linear_fwd(a, f32, s));
+    return launched(linear_few(a, false) ? launch_linear_few(a, false, f32, s) : launch_linear_fwd(a, f32, s));
 }
 
 dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, int32_t act,
@@ -394,7 +390,8 @@ dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, 
     a.qm = map_of(*vdx, vdx->C);
     a.act = act;
     (void)hipGetLastError();
-    return launched(launch_linear_bwd(a, f32, static_cast<hipStream_t>(stream)));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return launched(linear_few(a, true) ? launch_linear_few(a, true, f32, s) : launch_linear_bwd(a, f32, s));
 }
 
 size_t dc_linear_bwd_filter_workspace_bytes(const dc_view* vx, const dc_view* vdy) {
