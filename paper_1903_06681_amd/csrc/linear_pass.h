@@ -116,7 +116,18 @@ __device__ __forceinline__ void store_half(const float (&v)[16], const View& t, 
     const int64_t skip = 5 * step;
     if (o0 + 32 <= rows) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip)) store1(reinterpret_cast<T*>(a), v[r]);
+        for (int r = 0; r < 16; r += 2, next(a, r % 4 ? step : skip)) {
+            if constexpr (sizeof(T) == 4) {
+                *reinterpret_cast<float*>(a) = v[r];
+                next(a, step);
+                *reinterpret_cast<float*>(a) = v[r + 1];
+            } else {
+                const uint32_t two = packed(r);      // one conversion, its halves stored
+                *reinterpret_cast<uint16_t*>(a) = uint16_t(two);
+                next(a, step);
+                *reinterpret_cast<uint16_t*>(a) = uint16_t(two >> 16);
+            }
+        }
     } else {
 #pragma unroll
         for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip))
@@ -169,11 +180,10 @@ __device__ __forceinline__ void apply_slope(float (&z)[N], float (&v)[N], int ac
     }
 }
 
-// A lane's 16 channels (first of the block: o0) of slot `slot`, summed up: what is
-// left to do and to store.
-template <bool BWD, int PER>
-__device__ __forceinline__ void epilogue(float (&v)[16], const LinearArgs& a, int slot, int o0, int lane) {
-    const Place p = place_of<PER>(a.s, slot);
+// A lane's 16 channels (first of the block: o0) of a pixel, summed up: what is left to do
+// and to store.
+template <bool BWD>
+__device__ __forceinline__ void epilogue(float (&v)[16], const LinearArgs& a, const Place& p, int o0, int lane) {
     const int pix = p.c.r * a.s.len + p.w, h = lane >> 5;
     if constexpr (BWD) {
         if (a.act != DC_ACT_NONE) {
@@ -242,6 +252,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
     // overran the registers and the instruction cache.
     constexpr int Q = TM * TN, ROOM = NST * S::BYTES / (S::TH * 64), PER = Q < ROOM ? Q : ROOM;
     char* mine = &lds[0][0] + wave * (PER * 4096) + lane * 16;
+    Place p;
     __syncthreads();
     static_for<0, (Q + PER - 1) / PER>([&](auto part) __attribute__((always_inline)) {
         constexpr int q0 = decltype(part)::value * PER, q1 = q0 + PER < Q ? q0 + PER : Q;
@@ -257,6 +268,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
 #pragma unroll 1
         for (int q = q0; q < q1; ++q) {
             const int o0 = tr * S::BM + row0 + 32 * (q % TM);
+            if (q % TM == 0) p = place_of<CL ? 1 : S::E>(a.s, tc * S::BN + col0 + 32 * (q / TM) + (lane & 31));
             if (o0 >= a.rows) continue;
             float v[16];
 #pragma unroll
@@ -265,7 +277,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) v[4 * g + r] = t[r];
             }
-            epilogue<BWD, CL ? 1 : S::E>(v, a, tc * S::BN + col0 + 32 * (q / TM) + (lane & 31), o0, lane);
+            epilogue<BWD>(v, a, p, o0, lane);
         }
     });
 }

@@ -87,25 +87,30 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_wgrad_kernel(LinWgradArg
     }
 }
 
-// The sums of the shares, in a fixed order: 64 results a workgroup, its four waves a
-// quarter of the shares each.  The last K results are db.
+// The sums of the shares, in a fixed order: 64 lanes of V results a workgroup, its four
+// waves a quarter of the shares each.  The last K results are db.  V: 4 where n and K are
+// multiples of it (16 shares of 2048 x 512: 17.0 us with V = 1).
+template <int V>
 __global__ __launch_bounds__(256) void linear_wgrad_sum_kernel(LinWgradArgs a) {
-    __shared__ float red[4][64];
+    typedef float fv __attribute__((ext_vector_type(V)));
+    __shared__ fv red[4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t n = int64_t(a.K) * a.C, all = n + (a.db ? a.K : 0);
-    const int64_t e = int64_t(blockIdx.x) * 64 + lane;
+    const int64_t e = (int64_t(blockIdx.x) * 64 + lane) * V;
     const bool in = e < all, bias = e >= n;
     const float* p = bias ? a.part + a.shares * n + (e - n) : a.part + e;
     const int64_t step = bias ? a.K : n;
     const int per = (a.shares + 3) / 4, i1 = min((wave + 1) * per, a.shares);
-    float s = 0;
+    fv s = 0;
+    if (in) {
 #pragma unroll 8
-    for (int i = wave * per; i < i1; ++i) s += in ? p[i * step] : 0.0f;
+        for (int i = wave * per; i < i1; ++i) s += *reinterpret_cast<const fv*>(p + i * step);
+    }
     red[wave][lane] = s;
     __syncthreads();
     if (wave != 0 || !in) return;
     s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
-    float* d = bias ? a.db + (e - n) : a.dw + e;
+    fv* d = reinterpret_cast<fv*>(bias ? a.db + (e - n) : a.dw + e);
     *d = a.accumulate ? *d + s : s;
 }
 
@@ -153,7 +158,10 @@ hipError_t launch_linear_wgrad(const LinWgradArgs& a, bool f32, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.shares == 1) return e;
     const int64_t all = int64_t(a.K) * a.C + (a.db ? a.K : 0);
-    hipLaunchKernelGGL(linear_wgrad_sum_kernel, dim3(unsigned((all + 63) / 64)), dim3(256), 0, s, a);
+    if (a.K % 4 == 0)
+        hipLaunchKernelGGL(linear_wgrad_sum_kernel<4>, dim3(unsigned((all + 255) / 256)), dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL(linear_wgrad_sum_kernel<1>, dim3(unsigned((all + 63) / 64)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
