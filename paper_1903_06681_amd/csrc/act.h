@@ -36,6 +36,7 @@ struct View {
     char* p;
     int64_t sn, sc, sh;
     int32_t dt;        // DC_F32, DC_BF16, DC_Q8; -1: absent
+    int32_t big;       // large enough to be stored past the caches (products)
 };
 
 // The pixels of a set of views, numbered sample by sample in rows of `len`: the

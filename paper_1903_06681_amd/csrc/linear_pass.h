@@ -114,20 +114,29 @@ __device__ __forceinline__ void store_half(const float (&v)[16], const View& t, 
         return;
     }
     const int64_t skip = 5 * step;
-    if (o0 + 32 <= rows) {
+    auto all = [&](auto stream) __attribute__((always_inline)) {
+        auto put = [&](auto f) __attribute__((always_inline)) {
+            if constexpr (decltype(stream)::value) __builtin_nontemporal_store(f, reinterpret_cast<decltype(f)*>(a));
+            else *reinterpret_cast<decltype(f)*>(a) = f;
+        };
 #pragma unroll
         for (int r = 0; r < 16; r += 2, next(a, r % 4 ? step : skip)) {
             if constexpr (sizeof(T) == 4) {
-                *reinterpret_cast<float*>(a) = v[r];
+                put(v[r]);
                 next(a, step);
-                *reinterpret_cast<float*>(a) = v[r + 1];
+                put(v[r + 1]);
             } else {
                 const uint32_t two = packed(r);      // one conversion, its halves stored
-                *reinterpret_cast<uint16_t*>(a) = uint16_t(two);
+                put(uint16_t(two));
                 next(a, step);
-                *reinterpret_cast<uint16_t*>(a) = uint16_t(two >> 16);
+                put(uint16_t(two >> 16));
             }
         }
+    };
+    if (o0 + 32 <= rows && t.big) {
+        all(std::true_type{});
+    } else if (o0 + 32 <= rows) {
+        all(std::false_type{});
     } else {
 #pragma unroll
         for (int r = 0; r < 16; ++r, next(a, r % 4 ? step : skip))

@@ -392,6 +392,64 @@ def test_linear_bwd_filter(shape, layout, dtype):
     R.close(db.cpu().double().numpy(), ys.sum((0, 2)), (M + 4) * R.EPS32 * np.abs(ys).sum((0, 2)), "db")
 
 
+# N, C, H, W, K: the largest blocks with whole slices, with a ragged end of everything (rows
+# off the alignment), results stored past the caches, a single slice
+LARGE = [(2, 136, 128, 128, 512), (1, 257, 181, 183, 515), (1, 64, 300, 300, 264), (1, 24, 512, 522, 40)]
+
+
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+@pytest.mark.parametrize("dtype,keep", [("f32", "f32"), ("bf16", "q8"), ("bf16", "f32")])
+def test_linear_large_blocks(shape, dtype, keep):
+    """As above, the references summed in 64 bits on the GPU."""
+    N, C, H, W, K = shape
+    g = torch.Generator(device="cuda")
+    g.manual_seed(18)
+
+    def dev(*s):
+        return torch.randn(*s, generator=g, device="cuda")
+
+    def rows(t):
+        return t.permute(1, 0, 2, 3).reshape(t.shape[1], -1).double()
+
+    def near(got, want, tol, what):
+        bad = (rows(got) - want).abs() - tol
+        assert not bool((bad > 0).any()), (what, float(bad.max()))
+
+    dt, rnd = R.DT[dtype], R.BF if dtype == "bf16" else 0
+    x, w, b, res = dev(N, C, H, W).to(dt), (dev(K, C) / C ** 0.5).to(dt), 0.3 * dev(K), dev(N, K, H, W).to(dt)
+    y = torch.full((N, K, H, W), float("nan"), dtype=dt, device="cuda")
+    h, dz = torch.empty_like(y), torch.empty_like(y)
+    kz = ckpt(N, K, H, W) if keep == "q8" else torch.empty(N, K, H, W, device="cuda")
+    vz = dc.View.q8(N, K, H, W) if keep == "q8" else V(kz)
+    dc.linear_fwd(V(x), x, w, b, dc.DC_ACT_SILU, V(res), res, vz, kz, V(y), y)
+    z, top = w.double() @ rows(x) + b.double()[:, None], w.double().abs() @ rows(x).abs() + b.double().abs()[:, None]
+    want = z * torch.sigmoid(z) + rows(res)
+    near(y, want, 1.13 * (C + 2) * R.EPS32 * top + 4e-7 * z.abs() + (rnd + 2 * R.EPS32) * want.abs(), "y")
+    if keep == "q8":
+        zf = torch.empty(N, K, H, W, device="cuda")
+        dc.ckpt_load(vz, kz, dc.DC_ACT_NONE, V(zf), zf)
+        full = torch.zeros(-(-K // 32) * 32, N * H * W, dtype=torch.float64, device="cuda")
+        full[:K] = z.abs()
+        power = torch.exp2(torch.floor(torch.log2(full.view(-1, 32, N * H * W).amax(1))))
+        near(zf, z, 2.0 ** -6 * power.repeat_interleave(32, 0)[:K] * (1 + 1e-5) + (C + 2) * R.EPS32 * top, "z8")
+        zs = rows(zf)
+    else:
+        near(kz, z, (C + 2) * R.EPS32 * top, "z")
+        zs = rows(kz)
+    dy, w2 = dev(N, C, H, W).to(dt), (dev(C, K) / K ** 0.5).to(dt)
+    dc.linear_bwd_data(V(dy), dy, w2, dc.DC_ACT_SILU, vz, kz, V(h), h, V(dz), dz)
+    p, ptop, sg = w2.double().t() @ rows(dy), w2.double().abs().t() @ rows(dy).abs(), torch.sigmoid(zs)
+    want = p * sg * (1 + zs * (1 - sg))
+    near(dz, want, 1.13 * (C + 2) * R.EPS32 * ptop + 1e-6 * p.abs() + (rnd + 2 * R.EPS32) * want.abs(), "dz")
+    near(h, zs * sg, 4e-7 * zs.abs() + (rnd + 2 * R.EPS32) * (zs * sg).abs(), "h")
+    dw, db = torch.empty(K, C, device="cuda"), torch.empty(K, device="cuda")
+    dc.linear_bwd_filter(V(x), x, V(res), res, dw, db, 0, ws(dc.linear_bwd_filter_workspace_bytes(V(x), V(res))))
+    want, top = rows(res) @ rows(x).t(), rows(res).abs() @ rows(x).abs().t()
+    # slices, shares and lanes cut the sum of N H W terms in pieces of at most 4096
+    assert bool(((dw.double() - want).abs() <= 4096 * R.EPS32 * top).all())
+    assert bool(((db.double() - rows(res).sum(1)).abs() <= 4096 * R.EPS32 * rows(res).abs().sum(1)).all())
+
+
 def test_linear_mixed_layouts():
     """Rows of channels in, a tile out, and the other way: one view decides nothing for the others."""
     g = rng(14)
