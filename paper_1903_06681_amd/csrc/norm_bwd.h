@@ -55,8 +55,11 @@ __global__ __launch_bounds__(512, LPX == 64 && R == 1 ? 3 : 2) void norm_bwd_ker
             for (int e = 0; e < E; ++e) *part_at(cb, e) = 0;
         });
     int par = 0;
-    // every wave of a workgroup takes the same number of turns
-    for (int g0 = blockIdx.x * a.pg; g0 < a.groups; g0 += a.grid * a.pg, par ^= 1) {
+    // Every wave of a workgroup takes the same number of turns.  Where a wave's rows are short,
+    // neighbours share an XCD, and their lines meet in its L2 (1024 channels on 32 x 14 x 14
+    // read 129 MB of memory for 32 MB otherwise: 48 us against 38).
+    const int first = LPX == 64 ? int(blockIdx.x) : xcd_range(blockIdx.x, a.grid);
+    for (int g0 = first * a.pg; g0 < a.groups; g0 += a.grid * a.pg, par ^= 1) {
         const int m = (g0 + l.pg) * LPX + l.px;
         const bool in = m < a.px.M;
         const int mm = min(m, a.px.M - 1);
