@@ -66,7 +66,8 @@ __device__ __forceinline__ uint4 keep16(uint4 v, int n) {
 }
 
 // 16 bytes a lane from memory to LDS, the lanes' one after the other from `to` (the
-// wave's).  Written out: the compiler would wait for it before any LDS read.
+// wave's).  Written out: the compiler would wait for it before any LDS read.  (The
+// compiler holds nothing in m0 across statements.)
 __device__ __forceinline__ void direct16(const void* p, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :: "s"(__builtin_amdgcn_readfirstlane(to)), "v"(p) : "memory");
@@ -93,30 +94,32 @@ __device__ __forceinline__ Chunk chunk_of(const Slots& s, int ci) {
 
 enum { WEIGHT, PIXEL, LONG };   // which way an operand is found: see Stage
 
-// The shape of a workgroup's block: BM x BN of the result, ROWB bytes of k a slice,
-// NST slices in LDS, WM x WN waves; OCC waves a SIMD that the registers leave room for.
-template <typename T_, int BM_, int BN_, int ROWB_, int NST_, int WM_, int WN_, int OCC_>
+static constexpr int kRow = 128;   // bytes of k a slice
+
+// The shape of a workgroup's block: BM x BN of the result, NST slices in LDS (2, or 1 where
+// there is only one), WM x WN waves; OCC waves a SIMD that the registers leave room for.
+template <typename T_, int BM_, int BN_, int NST_, int WM_, int WN_, int OCC_>
 struct Shape {
     typedef T_ T;
-    static constexpr int BM = BM_, BN = BN_, ROWB = ROWB_, NST = NST_, WM = WM_, WN = WN_, OCC = OCC_;
-    static constexpr int E = 16 / int(sizeof(T)), BK = ROWB / int(sizeof(T));
-    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32, GROUPS = ROWB / 32;
-    static constexpr int ABYTES = BM * ROWB, BYTES = (BM + BN) * ROWB;
+    static constexpr int BM = BM_, BN = BN_, NST = NST_, WM = WM_, WN = WN_, OCC = OCC_;
+    static constexpr int E = 16 / int(sizeof(T)), BK = kRow / int(sizeof(T));
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32, GROUPS = kRow / 32;
+    static constexpr int ABYTES = BM * kRow, BYTES = (BM + BN) * kRow;
     static constexpr int TH = 64 * WM * WN;
 };
 
-// ---- staging of one operand's slice: R rows by ROWB bytes of k.
+// ---- staging of one operand's slice: R rows by 128 bytes of k.
 //   WEIGHT  a matrix, rows [row][k] (RK) or [k][row] (KR)
 //   PIXEL   rows are slots: k the channels' planes (KR), or contiguous (RK: rows of channels)
 //   LONG    k runs over the slots, rows are channels: planes (RK), or rows of channels (KR)
 // A thread's chunks of 16 bytes follow each other in LDS at a distance of the
 // workgroup; which chunk of memory they hold is permuted, so that LDS is written in
 // order (as direct loads must) and read without bank conflicts.
-template <typename T, int KIND, int SRC, int R, int ROWB, int TH>
+template <typename T, int KIND, int SRC, int R, int TH>
 struct Stage {
     static constexpr int E = 16 / int(sizeof(T));
-    static constexpr int CPR = KIND == RK ? ROWB / 16 : R / E;  // chunks of an LDS row
-    static constexpr int U = R * ROWB / 16 / TH;       // chunks a thread
+    static constexpr int CPR = KIND == RK ? kRow / 16 : R / E;  // chunks of an LDS row
+    static constexpr int U = R * kRow / 16 / TH;       // chunks a thread
     static constexpr int STEP = TH / CPR;              // LDS rows between them
     // pointers a thread keeps: one for all chunks where they lie at equal distances
     static constexpr int P = SRC == PIXEL && KIND == RK ? U : 1;
@@ -127,7 +130,7 @@ struct Stage {
 
     // the permutation of an LDS row's chunks; the same for all rows of a thread
     __device__ __forceinline__ static int mix(int row) {
-        if constexpr (KIND == RK) return ROWB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;   // 16 lanes, 256 bytes a cycle
+        if constexpr (KIND == RK) return (row >> 1) & 7;   // 16 lanes, 256 bytes a cycle
         else if constexpr (sizeof(T) == 2) return R >= 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
         else return 0;
     }
@@ -230,9 +233,9 @@ struct Stage {
 // ---- fragments.  k-group g: 16 (bf16) or 8 (fp32) values of k.  bf16: lane l
 // holds row l % 32, k 8 (l / 32) .. + 7.  fp32: k 4 (l / 32) + i for i = 0 .. 3,
 // one matrix instruction each.
-template <typename T, int KIND, int R, int ROWB, int TH>
+template <typename T, int KIND, int R, int TH>
 __device__ __forceinline__ void fragment(uint4& f, const char* lds, int row0, int g, int lane) {
-    typedef Stage<T, KIND, WEIGHT, R, ROWB, TH> S;
+    typedef Stage<T, KIND, WEIGHT, R, TH> S;
     const int h = lane >> 5, r = lane & 31;
     if constexpr (KIND == RK) {
         f = *reinterpret_cast<const uint4*>(lds + S::lds_at(row0 + r, 2 * g + h));
@@ -272,20 +275,19 @@ __device__ __forceinline__ void multiply(f32x16_t& acc, const uint4& a, const ui
 // A wave reads the next k-group's fragments while it multiplies the last read one's, also
 // from one slice to the next: before a slice's last group every wave has read all of it
 // (one barrier a slice), so its buffer is free and the next one's is in place.  DIRECT:
-// slices come straight into LDS, NST of them at a time; else through registers, two.
-// NST = 1: there is only one slice.
+// slices come straight into LDS; else through registers.
 template <typename S, int AK, int BK_, bool DIRECT, typename SA, typename SB, typename F>
 __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const SA& sa, const SB& sb, const Operand& oa,
                                           const Operand& ob, const Slots& s, int k0, int k1, char (*lds)[S::BYTES], int row0,
                                           int col0, int lane, F&& seen) {
     typedef typename S::T T;
-    constexpr int NST = DIRECT || S::NST == 1 ? S::NST : 2, LOADS = SA::U + SB::U;
+    constexpr int NST = S::NST;
     uint4 fa[2][S::TM], fb[2][S::TN];
     auto read = [&](int to, const char* a, int g) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i) fragment<T, AK, S::BM, S::ROWB, S::TH>(fa[to][i], a, row0 + 32 * i, g, lane);
+        for (int i = 0; i < S::TM; ++i) fragment<T, AK, S::BM, S::TH>(fa[to][i], a, row0 + 32 * i, g, lane);
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) fragment<T, BK_, S::BN, S::ROWB, S::TH>(fb[to][j], a + S::ABYTES, col0 + 32 * j, g, lane);
+        for (int j = 0; j < S::TN; ++j) fragment<T, BK_, S::BN, S::TH>(fb[to][j], a + S::ABYTES, col0 + 32 * j, g, lane);
     };
     auto multiply_group = [&](int from) __attribute__((always_inline)) {
 #pragma unroll
@@ -319,31 +321,19 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
         sa.store(va, lds[buf]);
         sb.store(vb, lds[buf] + S::ABYTES);
     };
-    // A step's loads have arrived.  Those of the NST - 2 steps after it may be on their way
-    // where all of them were issued: chunks past an end are fewer loads.
-    auto arrived = [&](int step) __attribute__((always_inline)) {
-        if (NST > 2 && whole && k0 + (step + NST - 1) * S::BK <= k1)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NST - 2) * LOADS) : "memory");
-        else
-            wait_direct();
-    };
-
     if constexpr (DIRECT) {
-#pragma unroll
-        for (int i = 0; i < (NST > 1 ? NST - 1 : 1); ++i)
-            if (i < n) fetch(i, i);
-        arrived(0);
+        fetch(0, 0);
+        wait_direct();
     } else {
         load(0);
         store(0);
         if (1 < n) load(1);
     }
     __syncthreads();
-    if (DIRECT && NST > 1 && NST - 1 < n) fetch(NST - 1, NST - 1);
+    if (DIRECT && NST > 1 && 1 < n) fetch(1, 1);
     read(0, lds[0], 0);
-    int buf = 0;
-    for (int step = 0; step < n; ++step) {
-        const int next = buf + 1 == NST ? 0 : buf + 1;
+    for (int step = 0, buf = 0; step < n; ++step, buf ^= 1) {
+        const int next = buf ^ 1;
         const bool more = step + 1 < n;
         if (!DIRECT && NST > 1 && more) {
             store(next);
@@ -354,16 +344,15 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
             if constexpr (g + 1 < S::GROUPS) {
                 read((g + 1) & 1, lds[buf], g + 1);
             } else if (NST > 1 && more) {
-                if (DIRECT) arrived(step + 1);
+                if (DIRECT) wait_direct();
                 __syncthreads();
-                if (DIRECT && step + NST < n) fetch(step + NST, buf);
+                if (DIRECT && step + 2 < n) fetch(step + 2, buf);
                 read(0, lds[next], 0);
             }
             __builtin_amdgcn_sched_barrier(0);
             multiply_group(g & 1);
             __builtin_amdgcn_sched_barrier(0);
         });
-        buf = next;
     }
 }
 

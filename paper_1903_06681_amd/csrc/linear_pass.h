@@ -232,14 +232,13 @@ template <typename S, bool BWD, bool CL, bool DIRECT>
 __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
     typedef typename S::T T;
     constexpr int AK = BWD ? KR : RK, PK = CL ? RK : KR, TM = S::TM, TN = S::TN;
-    constexpr int NST = DIRECT || S::NST == 1 ? S::NST : 2;
-    __shared__ __align__(16) char lds[NST][S::BYTES];
+    __shared__ __align__(16) char lds[S::NST][S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // blocks of one column range follow each other on an XCD: they read the same pixels
     const int id = xcd_range(blockIdx.x, a.tr * a.tc);
     const int tc = id / a.tr, tr = id - tc * a.tr;
-    Stage<T, AK, WEIGHT, S::BM, S::ROWB, S::TH> sa;
-    Stage<T, PK, PIXEL, S::BN, S::ROWB, S::TH> sb;
+    Stage<T, AK, WEIGHT, S::BM, S::TH> sa;
+    Stage<T, PK, PIXEL, S::BN, S::TH> sb;
     sa.init(a.a, a.s, tr * S::BM);
     sb.init(a.b, a.s, tc * S::BN);
     f32x16_t acc[TM][TN];
@@ -259,7 +258,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
     // The blocks of 32 x 32 pass through the wave's share of LDS, a lane's values back to
     // the lane: a loop at run time instead of one copy of the epilogue per block, which
     // overran the registers and the instruction cache.
-    constexpr int Q = TM * TN, ROOM = NST * S::BYTES / (S::TH * 64), PER = Q < ROOM ? Q : ROOM;
+    constexpr int Q = TM * TN, ROOM = S::NST * S::BYTES / (S::TH * 64), PER = Q < ROOM ? Q : ROOM;
     char* mine = &lds[0][0] + wave * (PER * 4096) + lane * 16;
     Place p;
     __syncthreads();
@@ -296,10 +295,10 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
 // with 128 x 256, 357 with 64 x 128).  Short sums are bound by what they store and by the
 // epilogue: more and smaller workgroups at a time (64 to 256 on 100352: 33 us against 40
 // and, with 256 x 256, 43).  Few pixels: blocks small enough for the chip to have some.
-template <typename T> using Large = Shape<T, 256, 256, 128, 2, 4, 2, 2>;
-template <typename T> using Middle = Shape<T, 64, 128, 128, 2, 1, 4, 3>;
-template <typename T> using Short = Shape<T, 64, 128, 128, 1, 1, 4, 4>;     // one slice: half the LDS
-template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2, 4>;
+template <typename T> using Large = Shape<T, 256, 256, 2, 4, 2, 2>;
+template <typename T> using Middle = Shape<T, 64, 128, 2, 1, 4, 3>;
+template <typename T> using Short = Shape<T, 64, 128, 1, 1, 4, 4>;     // one slice: half the LDS
+template <typename T> using Small = Shape<T, 64, 64, 2, 2, 2, 4>;
 
 template <typename S, bool BWD>
 static void launch_shape(LinearArgs a, hipStream_t s) {

@@ -30,15 +30,15 @@ template <typename S, bool CL, bool DIRECT>
 __global__ __launch_bounds__(S::TH, S::OCC) void linear_wgrad_kernel(LinWgradArgs a) {
     typedef typename S::T T;
     constexpr int KIND = CL ? KR : RK, TM = S::TM, TN = S::TN;
-    __shared__ __align__(16) char lds[DIRECT ? S::NST : 2][S::BYTES];
+    __shared__ __align__(16) char lds[S::NST][S::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int blocks = a.tr * a.tc;
     // the blocks of a share follow each other on an XCD: they read the same pixels
     const int id = xcd_range(blockIdx.x, blocks * a.shares);
     const int share = id / blocks, blk = id - share * blocks;
     const int tr = blk / a.tc, tc = blk - tr * a.tc;
-    Stage<T, KIND, LONG, S::BM, S::ROWB, S::TH> sa;
-    Stage<T, KIND, LONG, S::BN, S::ROWB, S::TH> sb;
+    Stage<T, KIND, LONG, S::BM, S::TH> sa;
+    Stage<T, KIND, LONG, S::BN, S::TH> sb;
     sa.init(a.a, a.s, tr * S::BM);
     sb.init(a.b, a.s, tc * S::BN);
     f32x16_t acc[TM][TN];
@@ -117,8 +117,8 @@ __global__ __launch_bounds__(256) void linear_wgrad_sum_kernel(LinWgradArgs a) {
 // Blocks of 256 x 256 where the result has them and each compute unit gets eight slices of
 // one, or of 64 x 64 (95 rows of channels, 160 x 320, fp32: 35 us in two large blocks);
 // shares so that one (two) workgroups a compute unit run, none with fewer than four slices.
-template <typename T> using Large = Shape<T, 256, 256, 128, 2, 4, 2, 2>;
-template <typename T> using Small = Shape<T, 64, 64, 128, 2, 2, 2, 4>;
+template <typename T> using Large = Shape<T, 256, 256, 2, 4, 2, 2>;
+template <typename T> using Small = Shape<T, 64, 64, 2, 2, 2, 4>;
 static bool large(const LinWgradArgs& a, bool f32) {
     const int64_t slices = int64_t(a.s.chunks) * a.s.per / (f32 ? 32 : 64);
     return a.K > 128 && a.C > 128 && int64_t((a.K + 255) / 256) * ((a.C + 255) / 256) * slices >= 8 * 256;
