@@ -1,6 +1,8 @@
 // Forward pass and input gradient of a product over channels: the tile loop of
 // linear.h with rows = output channels and columns = slots (pixels), and the
-// epilogue in registers.
+// epilogue in registers.  Bound: memory for short sums (64 to 256 channels on 100352
+// pixels, z in 8 bits, 90 MB: 29 us); for long ones the tile loop and the stores, one
+// after the other (512 to 2048 on 65536, 137 GFLOP, 474 MB: 293 us).
 //
 // In the result of the matrix instruction a lane holds one pixel's 16 of a block's
 // 32 channels (its partner, 32 lanes on, the others): bias, activation, its slope
@@ -293,8 +295,9 @@ __global__ __launch_bounds__(S::TH, S::OCC) void linear_kernel(LinearArgs a) {
 // Long sums over many pixels: the largest block, whose operands are read least often (512
 // channels to 2048 on 65536 pixels, forward with gelu and z in 8 bits, 300 us against 338
 // with 128 x 256, 357 with 64 x 128).  Short sums are bound by what they store and by the
-// epilogue: more and smaller workgroups at a time (64 to 256 on 100352: 33 us against 40
-// and, with 256 x 256, 43).  Few pixels: blocks small enough for the chip to have some.
+// epilogue: more and smaller workgroups at a time (64 to 256 on 100352, stored through the
+// caches: 33 us against 40 with 128 x 256 and 43 with 256 x 256; 29 past them).  Few
+// pixels: blocks small enough for the chip to have some.
 template <typename T> using Large = Shape<T, 256, 256, 2, 4, 2, 2>;
 template <typename T> using Middle = Shape<T, 64, 128, 2, 1, 4, 3>;
 template <typename T> using Short = Shape<T, 64, 128, 1, 1, 4, 4>;     // one slice: half the LDS

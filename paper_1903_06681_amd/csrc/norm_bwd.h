@@ -8,7 +8,9 @@
 // sums: the 64 products of a block are summed over the wave's pixels by halving
 // (each step a lane gives away half of its values), 63 exchanges for 64 sums, which
 // leaves one register a block to carry along a workgroup's pixels; the workgroups'
-// sums are added in order by a second launch.  No atomics.
+// sums are added in order by a second launch.  No atomics.  4 x 64 x 256 x 256
+// from the checkpoint, skip path added, u formed again (151 MB): 46 to 50 us and 5 for the
+// second launch; three waves a SIMD (four do not fit the registers: 111 us with scratch).
 #pragma once
 
 #include "norm.h"
