@@ -83,10 +83,16 @@ bool norm_plan(NormArgs& a, bool backward) {
     a.held = held <= 1 ? 1 : held == 2 && !a.cl && !(backward && a.lpx == 16) ? 2 : 0;   // as registers allow
     a.groups = int((int64_t(a.px.M) + a.lpx - 1) / a.lpx);
     // enough workgroups for the chip first, then up to four waves each (more would not fit
-    // the registers evenly)
-    a.pg = std::max(1, std::min(4 / a.nw, a.groups / 512));
+    // the registers evenly).  Backward launches only what is resident and a turn more costs a
+    // whole one, so it rounds up: 56 channels on 3 x 198 x 47 bf16 in one turn 17.5 us, in
+    // two 26.8; 64 on 1 x 150 x 160 11.7 and 17.2
+    a.pg = std::max(1, std::min(4 / a.nw, backward ? (a.groups + 511) / 512 : a.groups / 512));
     a.grid = (a.groups + a.pg - 1) / a.pg;
-    if (backward) a.grid = std::min(a.grid, a.lpx == 64 && a.held == 1 && a.nw <= 4 ? 768 : 512);   // what is resident at a time
+    // What is resident at a time: 12 or 8 waves a compute unit.  Eight-wave workgroups of 256
+    // channels on 4 x 128 x 128: 256 of them 45.5 us, 512 49.2.  No more than three workgroups:
+    // four of three waves (96 channels, 4 x 200 x 200) 48.4 us, three 41.0.
+    const int waves_cu = a.lpx == 64 && a.held == 1 ? 12 : 8;
+    if (backward) a.grid = std::min(a.grid, 256 * std::clamp(waves_cu / (a.nw * a.pg), 1, 3));
     return true;
 }
 
