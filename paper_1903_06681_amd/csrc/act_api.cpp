@@ -353,7 +353,7 @@ dc_status dc_linear_fwd(const dc_view* vx, const void* x, const void* w, const f
     a.act = act;
     (void)hipGetLastError();
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return launched(linear_few(a, false) ? launch_linear_few(a, false, f32, s) : launch_linear_fwd(a, f32, s));
+    return launched(linear_few(a, false, f32) ? launch_linear_few(a, false, f32, s) : launch_linear_fwd(a, f32, s));
 }
 
 dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, int32_t act,
@@ -398,7 +398,7 @@ dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, 
     a.act = act;
     (void)hipGetLastError();
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return launched(linear_few(a, true) ? launch_linear_few(a, true, f32, s) : launch_linear_bwd(a, f32, s));
+    return launched(linear_few(a, true, f32) ? launch_linear_few(a, true, f32, s) : launch_linear_bwd(a, f32, s));
 }
 
 size_t dc_linear_bwd_filter_workspace_bytes(const dc_view* vx, const dc_view* vdy) {

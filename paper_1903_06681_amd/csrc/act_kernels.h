@@ -63,7 +63,7 @@ struct LinearArgs {
     int32_t tr, tc;        // blocks along rows and columns
 };
 hipError_t launch_linear_fwd(const LinearArgs& a, bool f32, hipStream_t s);
-bool linear_few(const LinearArgs& a, bool bwd);    // too few blocks of pixels: a kernel of its own
+bool linear_few(const LinearArgs& a, bool bwd, bool f32);    // too few blocks of pixels: a kernel of its own
 hipError_t launch_linear_few(const LinearArgs& a, bool bwd, bool f32, hipStream_t s);
 hipError_t launch_linear_bwd(const LinearArgs& a, bool f32, hipStream_t s);
 

@@ -133,12 +133,17 @@ static int pixels_in(const LinearArgs& a) {
     return a.s.chunks / int(a.s.dsample.d) * (int(a.s.dsample.d) / a.s.cpr * a.s.len);
 }
 
-// Up to 64 pixels, or fewer than 32 blocks of the tile loop to share a long sum.  z in 8
-// bits is written 32 channels at a time: the tile loop's.
-bool linear_few(const LinearArgs& a, bool bwd) {
+// Up to 64 pixels, or a long sum with few blocks of the tile loop to share it.  Forward
+// where the loop's slices are dear (fp32's matrix rate, operands staged through registers):
+// up to 64 blocks, a workgroup a compute unit here.  fp32, 1024 channels to 256 on 32 x 32
+// 14.3 us, the tile loop's 24.6; 512 to 128 on 4096 pixels (128 blocks) 18.6 and 14.5.  bf16,
+// 1024 to 128 on 8 x 14 x 15 (not on 16 bytes) 11.3 and 14.5, but 2048 to 256 on 32 x 32
+// 16.4 and 13.0.  z in 8 bits is written 32 channels at a time: the tile loop's.
+bool linear_few(const LinearArgs& a, bool bwd, bool f32) {
     if (!bwd && a.z.dt == DC_Q8) return false;
     const int64_t M = pixels_in(a);
-    return M <= 64 || (a.a.red >= 256 && (a.rows + 63) / 64 * ((M + 63) / 64) < 32);
+    const int limit = !bwd && (f32 || !a.direct) ? 64 : 31;
+    return M <= 64 || (a.a.red >= 256 && (a.rows + 63) / 64 * ((M + 63) / 64) <= limit);
 }
 
 template <typename T, bool BWD, bool CL>

@@ -232,6 +232,17 @@ def test_norm_bwd(shape, layout, types):
             (np.abs(dus) * exh).sum((0, 2)), "dgamma")
 
 
+# between 512 and 2048 groups of 16 pixels (four of a row's): two to four a workgroup, one turn
+TURNS = [((1, 40, 107, 93), "dense"), ((1, 70, 120, 161), "padded"), ((3, 56, 98, 97), "gaps"), ((9000, 100, 1, 1), "rows"),
+         ((2500, 520, 1, 1), "slice")]
+
+
+@pytest.mark.parametrize("shape,layout", TURNS, ids=str)
+@pytest.mark.parametrize("types", ["f32-f32-f32", "q8-bf16-bf16"])
+def test_norm_bwd_pixel_groups_of_a_workgroup(shape, layout, types):
+    test_norm_bwd(shape, layout, types)
+
+
 def test_norm_bwd_many_pixels_is_the_same_twice():
     """More pixel groups than workgroups: every workgroup takes several turns; fixed order."""
     g = rng(6)
@@ -316,6 +327,16 @@ def test_linear_fwd(shape, layout, dtype, out, act, res):
         (R.BF * np.abs(want) if out == "bf16" else 0)
     R.close(R.f64(y), want, tol, "y")
     assert R.untouched(y, mem)
+
+
+# long sums with 54 to 64 blocks of 64 x 64 results to share them
+FEW = [((2, 300, 23, 29, 130), "dense"), ((1, 1030, 33, 31, 200), "gaps"), ((1100, 260, 1, 1, 130), "rows"), ((1100, 263, 1, 1, 130), "slice")]
+
+
+@pytest.mark.parametrize("shape,layout", FEW, ids=str)
+@pytest.mark.parametrize("dtype,out,act,res", [("f32", "f32", "gelu", "f32"), ("bf16", "bf16", "silu", "bf16")])
+def test_linear_fwd_long_sums_few_blocks(shape, layout, dtype, out, act, res):
+    test_linear_fwd(shape, layout, dtype, out, act, res)
 
 
 @pytest.mark.parametrize("shape,layout", PLAYOUTS, ids=str)
