@@ -413,6 +413,13 @@ def test_linear_bwd_filter(shape, layout, dtype):
     R.close(db.cpu().double().numpy(), ys.sum((0, 2)), (M + 4) * R.EPS32 * np.abs(ys).sum((0, 2)), "db")
 
 
+@pytest.mark.parametrize("shape,layout", [((2100, 1090, 1, 1, 1010), "rows"), ((1, 1090, 42, 51, 1010), "padded")], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_linear_bwd_filter_two_shares(shape, layout, dtype):
+    """288 blocks of 64 x 64 results, 33 slices and more."""
+    test_linear_bwd_filter(shape, layout, dtype)
+
+
 # N, C, H, W, K: the largest blocks with whole slices, with a ragged end of everything (rows
 # off the alignment), results stored past the caches, a single slice
 LARGE = [(2, 136, 128, 128, 512), (1, 257, 181, 183, 515), (1, 64, 300, 300, 264), (1, 24, 512, 522, 40)]
