@@ -318,6 +318,10 @@ typedef struct {
     int32_t dtype;         /* DC_F32, DC_BF16 or DC_Q8 */
 } dc_view;
 
+/*
+ * max(z, 0), z Phi(z) with the normal distribution's Phi, z / (1 + e^-z).  +infinity
+ * stays and NaN stays; at -infinity relu is 0, the other two NaN (-infinity times 0).
+ */
 typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_GELU = 2, DC_ACT_SILU = 3 } dc_activation;
 
 /*

@@ -77,8 +77,10 @@ __device__ __forceinline__ void store1(__bf16* p, float v) { *p = static_cast<__
 // coefficients of Abramowitz and Stegun, Handbook of Mathematical Functions
 // (1964), 7.1.26 (here halved, p over sqrt 2): |error| <= 1.5e-7, a rounding of fp32
 // near 1.  Twenty issue slots a value, eight of them the exponential and the
-// reciprocal: an epilogue's vector operations weigh as much as its matrix ones.
-struct Normal { float tail, e; };   // Phi(-|z|), e^(-z^2 / 2)
+// reciprocal: an epilogue's vector operations weigh as much as its matrix ones.  The
+// value is z times Phi(z) as written: +infinity stays (z less |z| times the tail would be
+// infinity times 0), and at -infinity it is NaN, as the formula's -infinity times 0.
+struct Normal { float phi, e; };   // Phi(z), e^(-z^2 / 2)
 __device__ __forceinline__ Normal normal(float z) {
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.23164189f, 1.0f));
     const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
@@ -86,7 +88,8 @@ __device__ __forceinline__ Normal normal(float z) {
     s = fmaf(s, t, 0.7107068705f);
     s = fmaf(s, t, -0.142248368f);
     s = fmaf(s, t, 0.127414796f);
-    return Normal{s * t * e, e};
+    const float tail = s * t * e;      // Phi(-|z|)
+    return Normal{z < 0 ? tail : 1.0f - tail, e};
 }
 __device__ __forceinline__ float logistic(float z) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
@@ -95,7 +98,7 @@ __device__ __forceinline__ float logistic(float z) {
 template <int ACT>
 __device__ __forceinline__ float act_fwd(float z) {
     if constexpr (ACT == DC_ACT_RELU) return z <= 0 ? 0.0f : z;   // NaN stays
-    if constexpr (ACT == DC_ACT_GELU) return fmaxf(z, 0.0f) - fabsf(z) * normal(z).tail;
+    if constexpr (ACT == DC_ACT_GELU) return z * normal(z).phi;
     if constexpr (ACT == DC_ACT_SILU) return z * logistic(z);
     return z;
 }
@@ -108,8 +111,8 @@ __device__ __forceinline__ void act_both(float z, float& v, float& d) {
         d = z <= 0 ? 0.0f : z > 0 ? 1.0f : z;
     } else if constexpr (ACT == DC_ACT_GELU) {
         const Normal n = normal(z);
-        v = fmaxf(z, 0.0f) - fabsf(z) * n.tail;
-        d = fmaf(z * 0.39894228f, n.e, z < 0 ? n.tail : 1.0f - n.tail);
+        v = z * n.phi;
+        d = fmaf(z * 0.39894228f, n.e, n.phi);
     } else if constexpr (ACT == DC_ACT_SILU) {
         const float s = logistic(z);
         v = z * s;

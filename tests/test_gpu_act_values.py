@@ -1,0 +1,101 @@
+"""Values at the ends of the range through the products' epilogues and the checkpoints:
+infinities, NaN and the largest numbers under every activation, in every block shape."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import act_ref as R
+import paper_1903_06681_amd as dc
+
+pytestmark = pytest.mark.gpu
+V = dc.View.of
+INF, NAN = float("inf"), float("nan")
+VALUES = [INF, -INF, NAN, 3e38, -3e38, 1e20, -1e20, 30.0, -30.0, 6.5, -6.5, 1.0, -1.0, 0.25, -0.25, 0.0]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    yield
+    torch.cuda.synchronize()
+
+
+def act(z, kind):
+    """One value.  At -infinity gelu and silu are -infinity times 0, as their formulas have it: NaN."""
+    if math.isnan(z) or kind == "none":
+        return z
+    if kind == "relu":
+        return max(z, 0.0)
+    if z == INF:
+        return INF
+    if z == -INF:
+        return NAN
+    if kind == "gelu":
+        return z * 0.5 * math.erfc(-z / math.sqrt(2))
+    return z / (1 + math.exp(-z)) if z > -700 else 0.0
+
+
+# N, C, H, W, K, layout: up to 64 pixels; long sums; blocks of 64 x 64, 64 x 128 in one and two slices, 256 x 256; rows
+PATHS = {"few": (1, 3, 4, 16, 40, "dense"), "few_long": (1, 300, 9, 16, 40, "dense"), "small": (2, 24, 20, 24, 72, "dense"),
+         "short": (1, 24, 256, 256, 72, "dense"), "middle": (1, 72, 256, 256, 72, "dense"), "large": (1, 136, 256, 256, 256, "dense"),
+         "few_row": (5, 64, 1, 1, 40, "rows"), "small_rows": (300, 64, 1, 1, 72, "rows"), "short_rows": (65536, 32, 1, 1, 64, "rows")}
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+def test_activations_of_infinities_and_the_largest_numbers(path, dtype, out):
+    """The first channel holds the value and weighs 1, the others hold zeros: z is the value."""
+    N, C, H, W, K, layout = PATHS[path]
+    M = N * H * W
+    values = torch.tensor(VALUES).to(R.DT[dtype])
+    picks = values[torch.arange(M) % len(VALUES)]
+    x, _ = R.tensor(layout, N, C, H, W, dtype, fill=0.0)
+    x[:, 0] = picks.view(N, H, W).cuda()
+    w = torch.ones(K, C, dtype=R.DT[dtype], device="cuda")
+    z, _ = R.tensor(layout, N, K, H, W, "f32")
+    y, _ = R.tensor(layout, N, K, H, W, out)
+    h, _ = R.tensor(layout, N, K, H, W, out)
+    dz, _ = R.tensor(layout, N, K, H, W, "f32")
+    dy, _ = R.tensor(layout, N, C, H, W, dtype, fill=1.0)
+    w2 = torch.ones(C, K, dtype=R.DT[dtype], device="cuda")
+
+    def compare(t, kind, what):
+        got = R.f64(t).transpose(1, 0, 2).reshape(K, M)
+        want = np.array([act(float(v), kind) for v in values])
+        # 4e-7 |z| as elsewhere, while the tail counts; a few roundings of the value, one of them to bf16
+        top = np.where(np.isfinite(want), np.abs(values.double().numpy()), 0)
+        tol = 4e-7 * np.minimum(top, 10) + 2e-6 * np.abs(want) + (R.BF * np.abs(want) if out == "bf16" and what != "z" else 0)
+        idx = np.arange(M) % len(VALUES)
+        R.close(got, np.broadcast_to(want[idx], got.shape), tol[idx], f"{what} {kind}")
+
+    for kind in ("none", "relu", "gelu", "silu"):
+        dc.linear_fwd(V(x), x, w, None, dc.ACT[kind], None, None, V(z), z, V(y), y)
+        compare(z, "none", "z")
+        compare(y, kind, "y")
+        if kind == "none":
+            continue
+        h.fill_(NAN)
+        dc.linear_bwd_data(V(dy), dy, w2, dc.ACT[kind], V(z), z, V(h), h, V(dz), dz)
+        compare(h, kind, "h")
+        # the slope of what is finite is finite, and C at the far right, 0 at the far left
+        got = R.f64(dz).transpose(1, 0, 2).reshape(K, M)
+        for i, v in enumerate(values[:min(M, len(VALUES))].tolist()):
+            if math.isfinite(v) and abs(v) >= 30:
+                assert np.allclose(got[:, i], C if v > 0 else 0, rtol=2e-6, atol=1e-8 * C), (kind, v)
+
+
+@pytest.mark.parametrize("kind", ["relu", "gelu", "silu"])
+def test_checkpoint_of_the_largest_numbers_under_an_activation(kind):
+    x = torch.zeros(1, 40, 1, 9)
+    for p, v in enumerate((3.4e38, -3.4e38, 1e30, -1e30, 2.0 ** -126, 0.0, 100.0, -100.0, INF)):
+        x[0, 0, 0, p] = v
+    t, y = x.cuda(), torch.empty(1, 40, 1, 9, device="cuda")
+    q = torch.empty(dc.ckpt_bytes(dc.View.q8(1, 40, 1, 9)), dtype=torch.uint8, device="cuda")
+    dc.ckpt_save(V(t), t, q)
+    dc.ckpt_load(dc.View.q8(1, 40, 1, 9), q, dc.ACT[kind], V(y), y)
+    kept = R.q8_decode(q, 1, 40, 9)
+    want = np.vectorize(lambda v: act(float(v), kind))(kept)
+    R.close(R.f64(y), want, 2e-6 * np.abs(want) + 1e-30, kind)
