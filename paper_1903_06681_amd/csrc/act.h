@@ -281,16 +281,16 @@ __device__ __forceinline__ void q8_store_block(char* q, const Q8Map& m, const Pi
     uint32_t w[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[j] = q8_pack(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3], per);
-    const uint32_t at = uint32_t(cb) * uint32_t(m.HW) + uint32_t(p.pix);
-    uint4* d = reinterpret_cast<uint4*>(q + p.n * m.qn + int64_t(at) * 32);
+    const int64_t at = int64_t(cb) * m.HW + p.pix;
+    uint4* d = reinterpret_cast<uint4*>(q + p.n * m.qn + at * 32);
     d[0] = make_uint4(w[0], w[1], w[2], w[3]);
     d[1] = make_uint4(w[4], w[5], w[6], w[7]);
     reinterpret_cast<uint8_t*>(q)[m.s0 + p.n * m.sn + at] = uint8_t(s);
 }
 
 __device__ __forceinline__ void q8_load_block(float (&v)[32], const char* q, const Q8Map& m, const Pixel& p, int cb) {
-    const uint32_t at = uint32_t(cb) * uint32_t(m.HW) + uint32_t(p.pix);
-    const uint4* d = reinterpret_cast<const uint4*>(q + p.n * m.qn + int64_t(at) * 32);
+    const int64_t at = int64_t(cb) * m.HW + p.pix;
+    const uint4* d = reinterpret_cast<const uint4*>(q + p.n * m.qn + at * 32);
     const uint4 a = d[0], b = d[1];
     const float step = q8_step(reinterpret_cast<const uint8_t*>(q)[m.s0 + p.n * m.sn + at]);
     const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};

@@ -99,3 +99,32 @@ def test_checkpoint_of_the_largest_numbers_under_an_activation(kind):
     kept = R.q8_decode(q, 1, 40, 9)
     want = np.vectorize(lambda v: act(float(v), kind))(kept)
     R.close(R.f64(y), want, 2e-6 * np.abs(want) + 1e-30, kind)
+
+
+def test_checkpoint_of_a_sample_with_more_blocks_than_32_bits_count():
+    """96 channels of 2^32 / 3 pixels: a block's number passes 2^32.  Rows are one row in memory."""
+    H, W = (1 << 20) + 1, 1366
+    vq = dc.View.q8(1, 96, H, W)
+    need, P = dc.ckpt_bytes(vq), H * W
+    assert 3 * P > 1 << 32 and P < 1 << 31
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < need + (4 << 30):
+        pytest.skip("needs 142 GB of the card")
+    g = torch.Generator()
+    g.manual_seed(1)
+    x = torch.randn(1, 96, 1, W, generator=g).cuda()
+    q = torch.empty(need, dtype=torch.uint8, device="cuda")
+    q[P * 32 * 3 - (1 << 20):P * 32 * 3].fill_(85)
+    q[P * 33 * 3 - 65536:].fill_(85)
+    dc.ckpt_save(V(x.expand(1, 96, H, W)), x, q)
+    row = R.q8_values(R.f64(x))[0]
+    scales = q[P * 32 * 3:P * 33 * 3]
+    for cb in range(3):
+        for first in (0, (1 << 30) - 100, (1 << 32) - 2 * P - 100, P - 2000):   # two starts, the place where the number wraps, the end
+            n, at = 2000, cb * P + first
+            v = q[at * 32:(at + n) * 32].view(torch.int8).view(n, 32).double()
+            s = torch.exp2(scales[at:at + n].double() - 133)
+            want = torch.from_numpy(row[32 * cb:32 * cb + 32]).t()[(first + torch.arange(n)) % W]
+            assert torch.equal((v * s[:, None]).cpu(), want), (cb, first)
+    del q, scales
+    torch.cuda.empty_cache()
