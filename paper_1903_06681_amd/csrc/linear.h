@@ -66,12 +66,14 @@ __device__ __forceinline__ uint4 keep16(uint4 v, int n) {
 }
 
 // 16 bytes a lane from memory to LDS, the lanes' one after the other from `to` (the
-// wave's).  Written out: the compiler would wait for it before any LDS read.  (The
-// compiler holds nothing in m0 across statements.)
+// wave's).  Written out: the compiler would wait for it before any LDS read.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"     // m0 is a reserved register; the compiler does write it
 __device__ __forceinline__ void direct16(const void* p, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "s"(__builtin_amdgcn_readfirstlane(to)), "v"(p) : "memory");
+                 :: "s"(__builtin_amdgcn_readfirstlane(to)), "v"(p) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ void wait_direct() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const char* p) {
     return uint32_t(uintptr_t((__attribute__((address_space(3))) const char*)p));
