@@ -42,13 +42,13 @@ static dc_status check_view(const dc_view* v, Use use, bool q8) {
         if (k.n > 1) end += double(k.n - 1) * double(k.s);
     }
     if (end > 4e18) return DC_ERR_TOO_LARGE;
-    if (use == WRITE) {        // nested without overlap
+    if (use == WRITE) {        // nested: a dimension's step lies past the last element of those inside it
         std::sort(d, d + 4, [](const Dim& a, const Dim& b) { return a.s < b.s || (a.s == b.s && a.n < b.n); });
         int64_t next = 1;
         for (const Dim& k : d) {
             if (k.n == 1) continue;
             if (k.s < next) return DC_ERR_SHAPE;
-            next = k.s * k.n;
+            next += (k.n - 1) * k.s;
         }
     }
     return DC_OK;

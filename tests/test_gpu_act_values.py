@@ -128,3 +128,36 @@ def test_checkpoint_of_a_sample_with_more_blocks_than_32_bits_count():
             assert torch.equal((v * s[:, None]).cpu(), want), (cb, first)
     del q, scales
     torch.cuda.empty_cache()
+
+
+# every second row of an odd tile, every third channel, planes that follow a last row directly
+STEPS = {"rows": lambda d: (full(d, 2, 40, 13, 18)[:, :, ::2], 2, 40, 7, 18), "channels": lambda d: (full(d, 2, 70, 6, 21)[:, ::3], 2, 24, 6, 21),
+         "tight": lambda d: (torch.as_strided(full(d, 1, 1, 1, 2 * 40 * 182), (2, 40, 8, 14), (40 * 182, 182, 24, 1)), 2, 40, 8, 14)}
+
+
+def full(dtype, *shape):
+    return torch.full(shape, NAN, dtype=R.DT[dtype], device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", STEPS)
+def test_results_in_slices_with_steps(name, dtype):
+    """The same bits as in a dense result, and nothing beside them."""
+    y, N, C, H, W = STEPS[name](dtype)
+    base = y._base
+    g = torch.Generator()
+    g.manual_seed(5)
+    x, w = torch.randn(N, C, H, W, generator=g).to(R.DT[dtype]).cuda(), torch.randn(C, C, generator=g).to(R.DT[dtype]).cuda()
+    q = torch.empty(dc.ckpt_bytes(dc.View.q8(N, C, H, W)), dtype=torch.uint8, device="cuda")
+    dc.ckpt_save(V(x), x, q)
+    calls = {"norm": lambda t: dc.norm_fwd(V(x), x, None, None, 1e-5, V(t), t),
+             "product": lambda t: dc.linear_fwd(V(x), x, w, None, dc.DC_ACT_GELU, None, None, None, None, V(t), t),
+             "gradient": lambda t: dc.linear_bwd_data(V(x), x, w, dc.DC_ACT_NONE, None, None, None, None, V(t), t),
+             "load": lambda t: dc.ckpt_load(dc.View.q8(N, C, H, W), q, dc.DC_ACT_NONE, V(t), t)}
+    for what, call in calls.items():
+        dense = torch.empty(N, C, H, W, dtype=R.DT[dtype], device="cuda")
+        base.fill_(NAN)
+        call(dense)
+        call(y)
+        assert torch.equal(y, dense), what
+        assert R.untouched(y, base), what
