@@ -350,7 +350,7 @@ dc_status dc_linear_fwd(const dc_view* vx, const void* x, const void* w, const f
     a.h.dt = -1;
     a.out = device_view(vy, y);
     a.qm = map_of(*vy, vy->C);
-    a.act = act;
+    a.act = act_code(act, vy->dtype == DC_F32);
     (void)hipGetLastError();
     hipStream_t s = static_cast<hipStream_t>(stream);
     return launched(linear_few(a, false, f32) ? launch_linear_few(a, false, f32, s) : launch_linear_fwd(a, f32, s));
@@ -395,7 +395,7 @@ dc_status dc_linear_bwd_data(const dc_view* vdy, const void* dy, const void* w, 
     a.h = device_view(vh, h);
     a.out = device_view(vdx, dx);
     a.qm = map_of(*vdx, vdx->C);
-    a.act = act;
+    a.act = act_code(act, vdx->dtype == DC_F32 || (h && vh->dtype == DC_F32));
     (void)hipGetLastError();
     hipStream_t s = static_cast<hipStream_t>(stream);
     return launched(linear_few(a, true, f32) ? launch_linear_few(a, true, f32, s) : launch_linear_bwd(a, f32, s));

@@ -36,9 +36,10 @@ __global__ __launch_bounds__(256) void ckpt_load_kernel(CkptArgs a) {
 
 template <typename T, bool CL>
 static void load_act(const CkptArgs& a, dim3 g, hipStream_t s) {
+    constexpr int kGelu = sizeof(T) == 4 ? int(ACT_GELU_F32) : int(DC_ACT_GELU);
     switch (a.act) {
         case DC_ACT_RELU: hipLaunchKernelGGL((ckpt_load_kernel<T, CL, DC_ACT_RELU>), g, dim3(256), 0, s, a); break;
-        case DC_ACT_GELU: hipLaunchKernelGGL((ckpt_load_kernel<T, CL, DC_ACT_GELU>), g, dim3(256), 0, s, a); break;
+        case DC_ACT_GELU: hipLaunchKernelGGL((ckpt_load_kernel<T, CL, kGelu>), g, dim3(256), 0, s, a); break;
         case DC_ACT_SILU: hipLaunchKernelGGL((ckpt_load_kernel<T, CL, DC_ACT_SILU>), g, dim3(256), 0, s, a); break;
         default: hipLaunchKernelGGL((ckpt_load_kernel<T, CL, DC_ACT_NONE>), g, dim3(256), 0, s, a);
     }

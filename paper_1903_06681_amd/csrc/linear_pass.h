@@ -167,6 +167,10 @@ __device__ __forceinline__ void apply_act(float (&v)[N], int act) {
 #pragma unroll
             for (int r = 0; r < N; ++r) v[r] = act_fwd<DC_ACT_SILU>(v[r]);
             break;
+        case ACT_GELU_F32:
+#pragma unroll
+            for (int r = 0; r < N; ++r) v[r] = act_fwd<ACT_GELU_F32>(v[r]);
+            break;
         default: break;
     }
 }
@@ -187,6 +191,7 @@ __device__ __forceinline__ void apply_slope(float (&z)[N], float (&v)[N], int ac
         case DC_ACT_RELU: each(std::integral_constant<int, DC_ACT_RELU>{}); break;
         case DC_ACT_GELU: each(std::integral_constant<int, DC_ACT_GELU>{}); break;
         case DC_ACT_SILU: each(std::integral_constant<int, DC_ACT_SILU>{}); break;
+        case ACT_GELU_F32: each(std::integral_constant<int, ACT_GELU_F32>{}); break;
         default: break;
     }
 }

@@ -161,3 +161,38 @@ def test_results_in_slices_with_steps(name, dtype):
         call(y)
         assert torch.equal(y, dense), what
         assert R.untouched(y, base), what
+
+
+def points(seed, n):
+    """Normal values of several scales, dense around 0 and out to +-30."""
+    g = torch.Generator()
+    g.manual_seed(seed)
+    z = torch.randn(5, n // 5, generator=g) * torch.tensor([0.01, 0.05, 0.3, 1.0, 8.0])[:, None]
+    return z.view(-1)
+
+
+def test_gelu_of_fp32_results_is_as_exact_as_fp32():
+    """Bounds from the roundings.  The tail is 2^(-1 - a R(a)) within 5.3e-9; its exponential an ulp off (2^-23 of
+    at most 1/2), its exponent's roundings weighed by a R 2^(-1 - a R) <= 0.27 (2^-23 of that), the sum with 1 and the
+    product with z 2^-24 each: 1.6e-7 |z| with the last of them taken at Phi <= 1.  The slope: Phi once more and
+    z phi(z) <= 0.25 by four operations: 4e-7."""
+    z = points(3, 40000)
+    x = z.view(1, 1, 100, 400).cuda()
+    w, w2 = torch.ones(2, 1, device="cuda"), torch.ones(1, 2, device="cuda")
+    y, h, dz, kz = (torch.empty(1, 2, 100, 400, device="cuda") for _ in range(4))
+    dc.linear_fwd(V(x), x, w, None, dc.DC_ACT_GELU, None, None, V(kz), kz, V(y), y)
+    assert torch.equal(kz[:, :1], x)
+    dy = torch.ones(1, 1, 100, 400, device="cuda")
+    dc.linear_bwd_data(V(dy), dy, w2, dc.DC_ACT_GELU, V(kz), kz, V(h), h, V(dz), dz)
+    zd = z.double()
+    want = zd * torch.special.ndtr(zd)
+    slope = torch.special.ndtr(zd) + zd * torch.exp(-zd * zd / 2) / math.sqrt(2 * math.pi)
+    for t, what in ((y, "y"), (h, "h")):
+        R.close(R.f64(t)[0, 0], want.numpy(), 1.6e-7 * zd.abs().numpy(), what)
+        assert torch.equal(t[:, 0], t[:, 1])
+    R.close(R.f64(dz)[0, 0], slope.numpy(), 4e-7, "slope")
+    assert torch.equal(h, y)
+    # at small scales the root of the mean square error stays within a rounding and a half of the values'
+    small = (zd.abs() < 0.3) & (zd != 0)
+    err = (y[0, 0].cpu().double().view(-1) - want)[small]
+    assert float(err.norm() / want[small].norm()) < 1.5 * R.EPS32
