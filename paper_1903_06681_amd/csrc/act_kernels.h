@@ -32,7 +32,7 @@ struct NormArgs {
     int32_t groups, grid;      // pixel groups, workgroups
     int32_t accumulate, cl;
 };
-bool norm_plan(NormArgs& a, bool backward);
+void norm_plan(NormArgs& a, bool backward);
 size_t norm_bwd_part_bytes(int M, int C);
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t s);

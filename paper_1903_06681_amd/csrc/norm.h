@@ -112,8 +112,9 @@ __device__ __forceinline__ void each_block(const NormArgs& a, const NormLane& l,
     }
 }
 
-// Launch K<type, LPX, R, CL> as planned (norm_plan keeps to these).
-#define DC_NORM_LAUNCH(KERNEL, a, s, ...)                                                                       \
+// Launch K<type, LPX, R, CL> as planned (norm_plan keeps to these).  HELD16: blocks that a
+// lane of a 16-pixel wave holds at most, 2 forward, 1 backward (which has twice the values).
+#define DC_NORM_LAUNCH(KERNEL, HELD16, a, s, ...)                                                               \
     do {                                                                                                        \
         const unsigned x_ = (a).grid < (1 << 22) ? (a).grid : 1 << 22;  /* threads of a dimension: 32 bits */   \
         const dim3 g_(x_, ((a).grid + x_ - 1) / x_), b_(64 * (a).nw * (a).pg);                                  \
@@ -121,8 +122,8 @@ __device__ __forceinline__ void each_block(const NormArgs& a, const NormLane& l,
         else if ((a).lpx == 64) hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 64, 2, false>), g_, b_, 0, s, a);       \
         else if ((a).lpx == 16 && !(a).cl && (a).held == 1)                                                     \
             hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 16, 1, false>), g_, b_, 0, s, a);                           \
-        else if ((a).lpx == 16 && !(a).cl && (a).held == 2)                                                     \
-            hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 16, 2, false>), g_, b_, 0, s, a);                           \
+        else if ((a).lpx == 16 && !(a).cl && (a).held == HELD16)                                                \
+            hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 16, HELD16, false>), g_, b_, 0, s, a);                      \
         else if ((a).lpx == 16 && !(a).cl) hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 16, 0, false>), g_, b_, 0, s, a);       \
         else if ((a).lpx == 16) hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 16, 1, true>), g_, b_, 0, s, a);        \
         else if ((a).held == 1) hipLaunchKernelGGL((KERNEL<__VA_ARGS__, 4, 1, true>), g_, b_, 0, s, a);         \

@@ -5,11 +5,11 @@ namespace dc {
 
 hipError_t launch_norm_bwd_f32(const NormArgs& a, hipStream_t s) {
     if (a.q)
-        DC_NORM_LAUNCH(norm_bwd_kernel, a, s, char, float);
+        DC_NORM_LAUNCH(norm_bwd_kernel, 1, a, s, char, float);
     else if (a.x.dt == DC_F32)
-        DC_NORM_LAUNCH(norm_bwd_kernel, a, s, float, float);
+        DC_NORM_LAUNCH(norm_bwd_kernel, 1, a, s, float, float);
     else
-        DC_NORM_LAUNCH(norm_bwd_kernel, a, s, __bf16, float);
+        DC_NORM_LAUNCH(norm_bwd_kernel, 1, a, s, __bf16, float);
     return hipGetLastError();
 }
 

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(512) void norm_fwd_kernel(NormArgs a) {
 // pixel lie next to each other, so that a wave reads whole rows.  Else 64 pixels
 // a wave, or 16 where that leaves the chip without work (fewer than 2048 waves of
 // 64 pixels and 32 channels) or the channels do not fit a workgroup's registers.
-bool norm_plan(NormArgs& a, bool backward) {
+void norm_plan(NormArgs& a, bool backward) {
     a.blocks = (a.C + 31) / 32;
     a.invC = 1.0f / float(a.C);
     const int64_t waves = (int64_t(a.px.M) + 63) / 64 * a.blocks;
@@ -93,14 +93,13 @@ bool norm_plan(NormArgs& a, bool backward) {
     // four of three waves (96 channels, 4 x 200 x 200) 48.4 us, three 41.0.
     const int waves_cu = a.lpx == 64 && a.held == 1 ? 12 : 8;
     if (backward) a.grid = std::min(a.grid, 256 * std::clamp(waves_cu / (a.nw * a.pg), 1, 3));
-    return true;
 }
 
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s) {
     if (a.x.dt == DC_F32)
-        DC_NORM_LAUNCH(norm_fwd_kernel, a, s, float);
+        DC_NORM_LAUNCH(norm_fwd_kernel, 2, a, s, float);
     else
-        DC_NORM_LAUNCH(norm_fwd_kernel, a, s, __bf16);
+        DC_NORM_LAUNCH(norm_fwd_kernel, 2, a, s, __bf16);
     return hipGetLastError();
 }
 
