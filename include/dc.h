@@ -309,7 +309,10 @@ const char* dc_status_string(int32_t status);
  * read with it; those values never reach a result.  Strides of tensors that are read may be 0
  * (broadcast); those of tensors that are written must not make elements overlap
  * (DC_ERR_SHAPE).  Outputs must not overlap inputs, except where said.
- * N H W is below 2^31 (DC_ERR_TOO_LARGE); offsets are 64-bit.
+ * Offsets are 64-bit.  Sizes (DC_ERR_TOO_LARGE past them): N H W up to 2^31 - 2^16, for
+ * products with every row of a tile that is not contiguous rounded up to 16 bytes; C up
+ * to 2^20; for products K C below 2^31 and at most 2^22 blocks of 128 channels (of the
+ * wider side) by 128 pixels.
  */
 #define DC_Q8 2   /* view dtype: a checkpoint in 8 bits (layout below, strides ignored) */
 typedef struct {

@@ -1,8 +1,9 @@
 // Forward pass and input gradient of a product over channels: the tile loop of
 // linear.h with rows = output channels and columns = slots (pixels), and the
 // epilogue in registers.  Bound: memory for short sums (64 to 256 channels on 100352
-// pixels, z in 8 bits, 90 MB: 29 us); for long ones the tile loop and the stores, one
-// after the other (512 to 2048 on 65536, 137 GFLOP, 474 MB: 293 us).
+// pixels, z in 8 bits, 90 MB: 29 us); for long ones the tile loop, the epilogue's vector
+// operations and the stores, one after the other (512 to 2048 on 65536, 137 GFLOP, 474 MB:
+// 285 to 310 us, of which 154, 90 and 95 each alone; its gradient 376 to 432).
 //
 // In the result of the matrix instruction a lane holds one pixel's 16 of a block's
 // 32 channels (its partner, 32 lanes on, the others): bias, activation, its slope

@@ -5,7 +5,7 @@
 // small and the sum long, so the slices are dealt out in shares, each with its own
 // sums in the workspace; a second launch adds the shares in order.  db is the
 // row sum of dy: the first column of blocks adds up the fragments that it
-// multiplies.  2048 x 512 over 65536 pixels (bf16, 137 GFLOP): 150 us, 900 TFLOP/s, and 13
+// multiplies.  2048 x 512 over 65536 pixels (bf16, 137 GFLOP): 154 us, 890 TFLOP/s, and 13
 // for the 16 shares; the loads from L2 bound the loop (1,150 TFLOP/s without them).
 #include <algorithm>
 
