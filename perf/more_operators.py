@@ -1,0 +1,501 @@
+"""A gated residual block between two convolutions, as timed cases: the gated
+feed-forward product, the join of a block's branch with its residual stream, and
+dropout whose mask is never stored.
+
+A case is one pass of a program that holds a tile, whole images, or rows of channels
+(H tokens of N sequences, W = 1):
+
+  gate  h = drop(act(Wg x + bg) * (Wu x + bu)); where `train`, the two products' sums
+        are kept (in 8 bits where `ckpt`) and the gradients at them follow from the
+        output's, with h formed again:
+          dh = drop(W2^T dy), dzg = dh * zu * act'(zg), dzu = dh * act(zg)
+  join  o = x + scale * gate * drop(post(y)), u = pre(o): the norm after a block, its
+        dropout, a gate a sample and a scale a channel, the residual sum and the norm
+        before the next block; where `train`, everything's gradients from those of u and o
+  drop  the dropout of an activation, then of its gradient with the same mask
+
+Norms are over the channels of a pixel: layer (x - mean) / sqrt(var + eps) or rms
+x / sqrt(mean x^2 + eps), times gamma, plus beta.
+
+The mask: channels 8 k .. 8 k + 7 of a pixel share the four words that Philox 4x32 with
+10 rounds (Salmon, Moraes, Dror and Shaw, SC 2011) gives for the counter (position,
+offset), position = ((sample * ceil(C / 8) + k) * rows + row) * columns + column in the
+WHOLE image, of which a tile is a part, and the key `seed`. Channel j of the eight
+takes 16 bits: word j // 2's lower half for even j, its upper half for odd ones. A value
+is dropped where these are below t = round(65536 p), and multiplied by 65536 / (65536 - t)
+where not.
+
+The 8-bit form: the 32 channels 32 k .. 32 k + 31 of a pixel share the power of two that
+the largest magnitude among them has, at least 2^-120; a value is the nearest multiple
+(ties to even) of a 64th of it, at most 127 of them.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+EPS = 1e-5
+#: limits of a drawn case, below those of the largest listed one
+MOST_FLOPS = {"bf16": 4e11, "f32": 2.5e10}
+MOST_BYTES = 5e8
+
+
+def _case(name, op, dtype, N, C, H, W, K=0, act="none", train=True, ckpt=False, halo=0, xdtype=None, post="none", pre="none",
+          gate=False, p=0.0, grid=1, rows=False):
+    c = {"op": op, "dtype": dtype, "N": N, "C": C, "H": H, "W": W, "K": K, "act": act, "train": train, "ckpt": ckpt, "halo": halo,
+         "xdtype": xdtype or dtype, "post": post, "pre": pre, "gate": gate, "p": p, "grid": grid, "rows": rows}
+    return {"name": name, **c} if name else c
+
+
+def listed():
+    return [
+        # serving: one token through a wide gated product, where the weights' way and launches count
+        _case("gate_token_bf16", "gate", "bf16", 1, 1024, 1, 1, K=4096, act="silu", train=False, rows=True),
+        # serving a few dozen tokens of an odd model in single precision
+        _case("gate_few_f32", "gate", "f32", 37, 520, 1, 1, K=1400, act="gelu", train=False, rows=True),
+        # a first-stage block on whole images, trained from 8 bits with dropout on the hidden values
+        _case("gate_56_bf16", "gate", "bf16", 32, 64, 56, 56, K=256, act="gelu", ckpt=True, p=0.1),
+        # an odd tile of a 2 x 2 grid, the interior of a padded one, the sums kept whole
+        _case("gate_ragged_bf16", "gate", "bf16", 3, 40, 93, 75, K=152, act="silu", halo=1, p=0.2, grid=2),
+        # the mesh model in single precision
+        _case("gate_mesh_f32", "gate", "f32", 1, 32, 512, 512, K=64, act="gelu"),
+        # the largest: 65536 tokens from 512 channels to twice 2048, as in a model of rows of channels
+        _case("gate_large_bf16", "gate", "bf16", 16, 512, 4096, 1, K=2048, act="silu", ckpt=True, rows=True),
+        # the smallest decomposed layer's tile: latency and launches count
+        _case("join_small_f32", "join", "f32", 2, 8, 16, 16, post="layer", pre="layer", gate=True, p=0.1),
+        # the 256 x 256 tile of a 4 x 4 grid: bf16 branch, fp32 residual stream
+        _case("join_tile_bf16", "join", "bf16", 4, 64, 256, 256, xdtype="f32", post="layer", pre="layer", p=0.1, grid=4),
+        # 8192 tokens of eight sequences, root-mean-square norms around the block, adaptive gates
+        _case("join_rows_bf16", "join", "bf16", 8, 1024, 1024, 1, post="rms", pre="rms", gate=True, p=0.1, rows=True),
+        # serving: the same for one new token of each of four sequences
+        _case("join_token_bf16", "join", "bf16", 4, 1024, 1, 1, post="rms", pre="rms", gate=True, train=False, rows=True),
+        # the 256 x 256 tile's activation and its gradient
+        _case("drop_tile_bf16", "drop", "bf16", 4, 64, 256, 256, p=0.1, grid=4),
+        # an odd tile in single precision, the last eight channels not full
+        _case("drop_ragged_f32", "drop", "f32", 3, 43, 93, 75, p=0.25, grid=2),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _channels(rng, lo, hi):
+    """Mostly whole groups of 8 to 64 channels, now and then any count."""
+    c, g = _log(rng, lo, hi), rng.choice((1, 8, 16, 32, 64))
+    return max(lo, min(hi, (c + g // 2) // g * g)) if c > g else c
+
+
+def _draw_one(rng):
+    op, dtype = rng.choice(("gate", "gate", "gate", "join", "join", "drop")), rng.choice(("f32", "bf16", "bf16"))
+    form, grid, halo = rng.choice(("tile", "image", "rows")), 1, 0
+    if form == "tile":       # a decomposed layer's tile
+        N, H, W, C, F, grid = rng.randint(1, 4), _log(rng, 16, 512), _log(rng, 16, 512), (8, 128), (8, 256), rng.choice((1, 2, 4))
+        halo = rng.choice((0, 1)) if op != "drop" else 0
+    elif form == "image":    # whole images, one GPU's samples
+        N, H, W, C, F = _log(rng, 1, 32), _log(rng, 2, 112), _log(rng, 2, 112), (16, 1024), (16, 2048)
+    else:                    # H tokens of N sequences, from a single one on
+        N, H, W, C, F = _log(rng, 1, 64), _log(rng, 1, 4096), 1, (64, 2048), (64, 2048)
+    train = rng.random() < 0.6
+    p = rng.choice((0.0, 0.1, round(rng.uniform(0.01, 0.6), 3)))
+    if op == "drop":
+        return _case(None, op, dtype, N, _channels(rng, *C), H, W, p=max(p, 0.05), grid=grid, rows=form == "rows")
+    if op == "gate":
+        # sums in 8 bits are for bf16 layers: in fp32 ones a sum that two orders of summation round to different
+        # eighth bits would make outputs differ by far more than fp32 sums do
+        return _case(None, op, dtype, N, _channels(rng, *C), H, W, K=_channels(rng, *F), act=rng.choice(("none", "relu", "gelu", "silu")),
+                     train=train, ckpt=train and dtype == "bf16" and rng.random() < 0.5, halo=halo, p=p if train else 0.0, grid=grid,
+                     rows=form == "rows")
+    return _case(None, op, dtype, N, _channels(rng, *C), H, W, xdtype=rng.choice(("f32", dtype)), post=rng.choice(("none", "layer", "rms")),
+                 pre=rng.choice(("layer", "rms")), gate=rng.random() < 0.5, train=train, halo=halo, p=p if train else 0.0, grid=grid,
+                 rows=form == "rows")
+
+
+def draw(rng):
+    while True:
+        c = _draw_one(rng)
+        w = work(c)
+        if w["flops"] <= MOST_FLOPS[c["dtype"]] and w["bytes"] <= MOST_BYTES:
+            return c
+
+
+def work(c):
+    m, e, ex = c["N"] * c["H"] * c["W"], 4 if c["dtype"] == "f32" else 2, 4 if c["xdtype"] == "f32" else 2
+    C, K = c["C"], c["K"]
+    if c["op"] == "gate":
+        kept = 2 * m * K * (33 / 32 if c["ckpt"] else e) if c["train"] else 0
+        b, f = e * (m * C + 2 * K * C + m * K) + 8 * K + kept, 4 * m * C * K
+        if c["train"]:       # dy, W2, the kept sums in; their gradients and h out
+            b, f = b + e * (m * C + K * C + 3 * m * K) + kept, f + 2 * m * C * K
+        return {"bytes": b, "flops": f}
+    if c["op"] == "join":
+        stats = m * 8 * ((c["post"] != "none") + (c["pre"] != "none"))
+        small = 4 * C * (1 + 2 * (c["post"] != "none") + 2 * (c["pre"] != "none") + (c["N"] if c["gate"] else 0))
+        b, f = m * C * (2 * e + 2 * ex) + small, m * C * 20          # y, x in; o, u out
+        if c["train"]:                                               # du, do, y, o in; dx, dy out
+            b, f = b + m * C * (3 * e + 3 * ex) + 2 * stats + 2 * small, f + m * C * 30
+        return {"bytes": b, "flops": f}
+    return {"bytes": 4 * m * C * e, "flops": 4 * m * C}
+
+
+def _tile(c, channels, dtype, halo):
+    """An empty tensor: rows of channels, dense planes, or the interior of a tile with a margin and 16-byte rows (its margin zeros)."""
+    if c["rows"]:
+        return torch.empty(c["N"], c["H"], channels, dtype=DTYPES[dtype], device="cuda").permute(0, 2, 1).unsqueeze(3)
+    if not halo:
+        return torch.empty(c["N"], channels, c["H"], c["W"], dtype=DTYPES[dtype], device="cuda")
+    per = 16 // DTYPES[dtype].itemsize
+    pitch = -(-(c["W"] + 2 * halo) // per) * per
+    t = torch.zeros(c["N"], channels, c["H"] + 2 * halo, pitch, dtype=DTYPES[dtype], device="cuda")
+    return t[:, :, halo:halo + c["H"], halo:halo + c["W"]]
+
+
+def prepare(c, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+
+    def filled(channels, dtype, halo=0, offset=0.0):
+        t = _tile(c, channels, dtype, halo)
+        spread = 0.5 + torch.rand(1, channels, 1, 1, generator=g, device="cuda")   # channels differ in scale and mean
+        t.copy_(randn(*t.shape).mul_(spread).add_(offset * randn(1, channels, 1, 1)))
+        return t
+
+    C, K, dt = c["C"], c["K"], DTYPES[c["dtype"]]
+    bits = random.Random(seed)
+    s = {"c": c, "seed": bits.getrandbits(63), "offset": bits.getrandbits(40)}
+    if c["op"] == "gate":
+        s["x"] = filled(C, c["dtype"], c["halo"])
+        s["w"], s["b"] = (randn(2 * K, C) / math.sqrt(C)).to(dt), 0.2 * randn(2 * K)
+        if c["train"]:
+            s["dy"], s["w2"] = filled(C, c["dtype"]), (randn(C, K) / math.sqrt(K)).to(dt)
+    elif c["op"] == "join":
+        s["y"], s["x"] = filled(C, c["dtype"], offset=0.5), filled(C, c["xdtype"], offset=0.5)
+        s["scale"], s["gate"] = 0.5 + 0.2 * randn(C), 1 + 0.3 * randn(c["N"], C) if c["gate"] else None
+        for k in ("post", "pre"):
+            s["gamma_" + k], s["beta_" + k] = (1 + 0.2 * randn(C), 0.2 * randn(C)) if c[k] != "none" else (None, None)
+        if c["train"]:
+            s["du"], s["do"] = filled(C, c["dtype"]), filled(C, c["xdtype"])
+    else:
+        s["x"], s["dy"] = filled(C, c["dtype"], offset=0.5), filled(C, c["dtype"])
+    if own:
+        _handles(s)
+    return s
+
+
+def _place(c):
+    """The tile's first row and column in the whole image, and the image's size: of a grid of tiles, the one in the middle."""
+    k = c["grid"] // 2
+    return k * c["H"], k * c["W"], c["grid"] * c["H"], c["grid"] * c["W"]
+
+
+def _handles(s):
+    """What a program of this library keeps beside its tensors: descriptors of their layout, outputs, checkpoints, workspaces."""
+    import paper_1903_06681_amd as dc
+    c = s["c"]
+    N, C, K, H, W = (c[k] for k in "NCKHW")
+
+    def out(name, channels, dtype="dtype", halo=0):
+        s[name] = _tile(c, channels, c[dtype], halo)
+
+    h0, w0, rows, cols = _place(c)
+    s["drop"] = dc.Drop(c["p"], s["seed"], s["offset"], h0=h0, w0=w0, H=rows, W=cols) if c["p"] else None
+    if c["op"] == "gate":
+        s["act"] = dc.ACT[c["act"]]
+        out("h", K)
+        if c["train"]:
+            out("h2", K), out("dz", 2 * K)
+            if c["ckpt"]:
+                q = s["vz"] = dc.View.q8(N, K, H, W)
+                s["zg"], s["zu"] = (torch.empty(dc.ckpt_bytes(q), dtype=torch.uint8, device="cuda") for _ in range(2))
+            else:
+                out("zg", K), out("zu", K)
+                s["vz"] = dc.View.of(s["zg"])
+    elif c["op"] == "join":
+        out("o", C, "xdtype"), out("u", C, halo=c["halo"])
+        for k in ("post", "pre"):
+            s[k] = dc.Norm(dc.NORM[c[k]], EPS, s["gamma_" + k], s["beta_" + k]) if c[k] != "none" else None
+        if c["train"]:
+            out("dx", C, "xdtype"), out("dy", C)
+            s["stat"] = torch.empty(4, N, H, W, device="cuda")
+            f = lambda *shape: torch.empty(*shape, device="cuda")   # noqa: E731
+            s["grads"] = dc.JoinGrads(scale=f(C), gate=f(N, C) if c["gate"] else None,
+                                      gamma_post=f(C) if s["post"] else None, beta_post=f(C) if s["post"] else None,
+                                      gamma_pre=f(C), beta_pre=f(C))
+    else:
+        out("y", C), out("dx", C)
+    for name in ("x", "y", "o", "u", "h", "h2", "dx", "dy", "do", "du", "dz"):
+        s["v" + name] = dc.View.of(s[name]) if s.get(name) is not None else None
+    if c["op"] == "join" and c["train"]:
+        s["ws"] = torch.empty(max(16, dc.join_bwd_workspace_bytes(s["vdy"], c["gate"])), dtype=torch.uint8, device="cuda")
+
+
+def run(s):
+    return _run_own(s) if own else _run_plain(s)
+
+
+def _run_own(s):
+    import paper_1903_06681_amd as dc
+    c = s["c"]
+    if c["op"] == "gate":
+        if not c["train"]:
+            dc.gate_fwd(s["vx"], s["x"], s["w"], s["b"], s["act"], None, None, None, None, s["vh"], s["h"])
+            return s["h"]
+        dc.gate_fwd(s["vx"], s["x"], s["w"], s["b"], s["act"], s["drop"], s["vz"], s["zg"], s["zu"], s["vh"], s["h"])
+        dc.gate_bwd_data(s["vdy"], s["dy"], s["w2"], s["act"], s["drop"], s["vz"], s["zg"], s["zu"], s["vh2"], s["h2"], s["vdz"], s["dz"])
+        kept = (None, None) if c["ckpt"] else (s["zg"], s["zu"])
+        return {"h": s["h"], "zg": kept[0], "zu": kept[1], "h2": s["h2"], "dz": s["dz"]}
+    if c["op"] == "join":
+        dc.join_fwd(s["vy"], s["y"], s["post"], s["scale"], s["gate"], s["drop"], s["vx"], s["x"], s["pre"], s["vo"], s["o"],
+                    s["vu"], s["u"], s.get("stat"))
+        if not c["train"]:
+            return {"o": s["o"], "u": s["u"]}
+        dc.join_bwd(s["vdu"], s["du"], s["vdo"], s["do"], s["vy"], s["y"], s["vo"], s["o"], s["stat"], s["post"], s["scale"], s["gate"],
+                    s["drop"], s["pre"], s["vdx"], s["dx"], s["vdy"], s["dy"], s["grads"], 0, s["ws"])
+        d = s["grads"]
+        return {"o": s["o"], "u": s["u"], "dx": s["dx"], "dy": s["dy"], "dscale": d.scale, "dgate": d.gate, "dgamma_post": d.gamma_post,
+                "dbeta_post": d.beta_post, "dgamma_pre": d.gamma_pre, "dbeta_pre": d.beta_pre}
+    dc.dropout(s["drop"], s["vx"], s["x"], s["vy"], s["y"])
+    dc.dropout(s["drop"], s["vdy"], s["dy"], s["vdx"], s["dx"])
+    return {"y": s["y"], "dx": s["dx"]}
+
+
+# ------------------------------------------------------------- the plain form
+
+def _flat(t):
+    return t.float().flatten(2)
+
+
+def _q8(x):
+    """The values that [N][C][pixels] stands for in 8 bits."""
+    n, ch, p = x.shape
+    b = torch.nn.functional.pad(x, (0, 0, 0, -ch % 32)).view(n, -1, 32, p)
+    e = (b.abs().amax(2, keepdim=True).view(torch.int32) >> 23).clamp_(min=7)
+    step, per = ((e - 6) << 23).view(torch.float32), ((260 - e) << 23).view(torch.float32)   # powers of two, per = 1 / step
+    return ((b * per).round_().clamp_(-127, 127) * step).view(n, -1, p)[:, :ch]
+
+
+def _drop(s, v):
+    """v [N][channels][pixels], dropped and scaled."""
+    c = s["c"]
+    t = round(65536 * c["p"])
+    if not t:
+        return v
+    n, ch, _ = v.shape
+    h0, w0, rows, cols = _place(c)
+    low = 0xFFFFFFFF
+
+    def at(n, dim):
+        return torch.arange(n, device="cuda").view([-1 if k == dim else 1 for k in range(4)])
+
+    pos = ((at(n, 0) * -(-ch // 8) + at(-(-ch // 8), 1)) * rows + h0 + at(c["H"], 2)) * cols + w0 + at(c["W"], 3)
+    w = [pos & low, pos >> 32, torch.full_like(pos, s["offset"] & low), torch.full_like(pos, s["offset"] >> 32)]
+    k0, k1 = s["seed"] & low, s["seed"] >> 32
+    for _ in range(10):      # products modulo 2^64: the bits above the lower 32 are the product's upper half
+        a, b = w[0] * 0xD2511F53, w[2] * 0xCD9E8D57
+        w = [((b >> 32) & low) ^ w[1] ^ k0, b & low, ((a >> 32) & low) ^ w[3] ^ k1, a & low]
+        k0, k1 = (k0 + 0x9E3779B9) & low, (k1 + 0xBB67AE85) & low
+    keep = torch.stack([half for x in w for half in ((x & 0xFFFF) >= t, (x >> 16) >= t)], 2)     # [N][groups][8][H][W]
+    return torch.where(keep.flatten(3).flatten(1, 2)[:, :ch], v * (65536 / (65536 - t)), 0.0)
+
+
+def _product(w, x):
+    """w [K][C] times every pixel of x [N][C][pixels]."""
+    return torch.matmul(x[:, :, 0], w.t())[:, :, None] if x.shape[2] == 1 else torch.matmul(w, x)
+
+
+def _act(z, act):
+    if act == "relu":
+        return z.clamp(min=0)
+    if act == "gelu":
+        return z * (0.5 + 0.5 * torch.erf(z * math.sqrt(0.5)))
+    return z * torch.sigmoid(z) if act == "silu" else z
+
+
+def _act_slope(z, act):
+    if act == "none":
+        return torch.ones_like(z)
+    if act == "relu":
+        return (z > 0).float()
+    if act == "gelu":
+        return 0.5 + 0.5 * torch.erf(z * math.sqrt(0.5)) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    sig = torch.sigmoid(z)
+    return sig * (1 + z * (1 - sig))
+
+
+def _norm(x, kind):
+    """The normed x and 1 / its deviation."""
+    d = x - x.mean(1, keepdim=True) if kind == "layer" else x
+    r = torch.rsqrt((d * d).mean(1, keepdim=True) + EPS)
+    return d * r, r
+
+
+def _norm_bwd(g, xh, r, kind):
+    m1 = g.mean(1, keepdim=True) if kind == "layer" else 0.0
+    return r * (g - m1 - xh * (g * xh).mean(1, keepdim=True))
+
+
+def _run_plain(s):
+    c = s["c"]
+    dt, xdt, shape = DTYPES[c["dtype"]], DTYPES[c["xdtype"]], (c["N"], -1, c["H"], c["W"])
+
+    def tile(t, dt=dt):
+        return t.to(dt).view(shape)
+
+    x = _flat(s["x"])
+    if c["op"] == "gate":
+        K = c["K"]
+        z = _product(s["w"].float(), x) + s["b"][:, None]
+        zg, zu = z[:, :K], z[:, K:]
+        h = tile(_drop(s, _act(zg, c["act"]) * zu))
+        if not c["train"]:
+            return h
+        kept = (None, None) if c["ckpt"] else (tile(zg), tile(zu))
+        zg, zu = (_q8(zg), _q8(zu)) if c["ckpt"] else (_flat(kept[0]), _flat(kept[1]))
+        dh = _drop(s, _product(s["w2"].float().t(), _flat(s["dy"])))
+        dz = torch.cat((dh * zu * _act_slope(zg, c["act"]), dh * _act(zg, c["act"])), 1)
+        return {"h": h, "zg": kept[0], "zu": kept[1], "h2": tile(_drop(s, _act(zg, c["act"]) * zu)), "dz": tile(dz)}
+    if c["op"] == "join":
+        y, sc = _flat(s["y"]), s["scale"][:, None]
+        if s["gate"] is not None:
+            gt = s["gate"][:, :, None]
+        else:
+            gt = torch.ones(1, 1, 1, device="cuda")
+        yh, ry = _norm(y, c["post"]) if c["post"] != "none" else (y, None)
+        v = _drop(s, s["gamma_post"][:, None] * yh + s["beta_post"][:, None] if c["post"] != "none" else y)
+        o = x + sc * gt * v
+        oh, ro = _norm(o, c["pre"])
+        out = {"o": tile(o, xdt), "u": tile(s["gamma_pre"][:, None] * oh + s["beta_pre"][:, None])}
+        if not c["train"]:
+            return out
+        du = _flat(s["du"])
+        do = _flat(s["do"]) + _norm_bwd(s["gamma_pre"][:, None] * du, oh, ro, c["pre"])
+        t = (do * v).sum(2)
+        dv = _drop(s, do * sc * gt)
+        post = c["post"] != "none"
+        dy = _norm_bwd(s["gamma_post"][:, None] * dv, yh, ry, c["post"]) if post else dv
+        out.update(dx=tile(do, xdt), dy=tile(dy), dscale=(t * gt[:, :, 0]).sum(0), dgate=s["scale"] * t if c["gate"] else None,
+                   dgamma_post=(dv * yh).sum((0, 2)) if post else None, dbeta_post=dv.sum((0, 2)) if post else None,
+                   dgamma_pre=(du * oh).sum((0, 2)), dbeta_pre=du.sum((0, 2)))
+        return out
+    return {"y": tile(_drop(s, x)), "dx": tile(_drop(s, _flat(s["dy"])))}
+
+
+# ------------------------------------------------------------- the definition in 64 bits
+
+def _mask(s, ch):
+    """What the pixels' channels are multiplied by, [pixels][ch]; by numpy, in the order of the definition."""
+    c = s["c"]
+    t = int(np.rint(65536 * np.float64(c["p"])))
+    N, H, W, G = c["N"], c["H"], c["W"], (ch + 7) // 8
+    h0, w0, rows, cols = _place(c)
+    n, h, w, k = np.ix_(np.arange(N), np.arange(h0, h0 + H), np.arange(w0, w0 + W), np.arange(G))
+    pos = np.asarray(((n * G + k) * rows + h) * cols + w, dtype=np.uint64)
+    mul = (np.uint64(0xD2511F53), np.uint64(0xCD9E8D57))
+    weyl = (np.uint32(0x9E3779B9), np.uint32(0xBB67AE85))
+    half, low = np.uint64(32), np.uint64(0xFFFFFFFF)
+    ctr = np.empty((4,) + pos.shape, dtype=np.uint32)
+    ctr[0], ctr[1] = pos & low, pos >> half
+    ctr[2], ctr[3] = s["offset"] & 0xFFFFFFFF, s["offset"] >> 32
+    key = np.array([s["seed"] & 0xFFFFFFFF, s["seed"] >> 32], dtype=np.uint32)
+    for _ in range(10):
+        p0, p1 = ctr[0].astype(np.uint64) * mul[0], ctr[2].astype(np.uint64) * mul[1]
+        ctr[0] = (p1 >> half).astype(np.uint32) ^ ctr[1] ^ key[0]
+        ctr[2] = (p0 >> half).astype(np.uint32) ^ ctr[3] ^ key[1]
+        ctr[1], ctr[3] = (p1 & low).astype(np.uint32), (p0 & low).astype(np.uint32)
+        key = key + np.array(weyl, dtype=np.uint32)
+    sixteen = np.ascontiguousarray(np.moveaxis(ctr, 0, -1)).view("<u2").reshape(N * H * W, G * 8)[:, :ch]
+    keep = torch.from_numpy(sixteen.astype(np.int32) >= t).to("cuda")
+    return keep.double() * (65536 / (65536 - t))
+
+
+def exact(c, seed):
+    s = prepare(c, seed)
+    N, C, H, W = c["N"], c["C"], c["H"], c["W"]
+
+    def rows(t):                      # pixels by channels
+        return t.permute(0, 2, 3, 1).reshape(N * H * W, -1).double()
+
+    def back(r):
+        return r.reshape(N, H, W, -1).permute(0, 3, 1, 2)
+
+    def eight_bits(r):
+        out = torch.empty_like(r)
+        for k in range(0, r.shape[1], 32):
+            b = r[:, k:k + 32]
+            top = b.abs().max(1, keepdim=True).values
+            step = (top / torch.frexp(top).mantissa).nan_to_num(0.0).clamp(min=2.0 ** -119) / 128   # top's own power of two
+            out[:, k:k + 32] = torch.clamp(torch.round(b / step), -127, 127) * step
+        return out
+
+    def act(z):
+        return {"none": lambda: z, "relu": lambda: torch.where(z > 0, z, 0 * z), "gelu": lambda: z * torch.special.ndtr(z),
+                "silu": lambda: z / (1 + torch.exp(-z))}[c["act"]]()
+
+    def slope(z):
+        if c["act"] == "gelu":
+            return torch.special.ndtr(z) + z * torch.exp(-z * z / 2) * (2 * math.pi) ** -0.5
+        if c["act"] == "silu":
+            e = torch.exp(-z)
+            return (1 + e + z * e) / (1 + e) ** 2
+        return torch.where(z > 0, 1.0, 0.0).double() if c["act"] == "relu" else torch.ones_like(z)
+
+    if c["op"] == "drop":
+        m = _mask(s, C)
+        return {"y": back(rows(s["x"]) * m), "dx": back(rows(s["dy"]) * m)}
+    x = rows(s["x"])
+    if c["op"] == "gate":
+        K = c["K"]
+        m = _mask(s, K) if c["p"] else 1.0
+        z = torch.addmm(s["b"].double(), x, s["w"].double().t())
+        g, u = z[:, :K], z[:, K:]
+        h = back(act(g) * u * m)
+        if not c["train"]:
+            return h
+        kept = (None, None) if c["ckpt"] else (back(g), back(u))
+        if c["ckpt"]:
+            g, u = eight_bits(g), eight_bits(u)
+        d = torch.mm(rows(s["dy"]), s["w2"].double()) * m
+        return {"h": h, "zg": kept[0], "zu": kept[1], "h2": back(act(g) * u * m), "dz": back(torch.hstack((d * u * slope(g), d * act(g))))}
+    m = _mask(s, C) if c["p"] else 1.0
+    a = s["scale"].double().expand(N, C)
+    b = a * s["gate"].double() if c["gate"] else a
+    b = b.repeat_interleave(H * W, 0)           # a factor a pixel and channel
+
+    def normed(t, kind):
+        mean = t.mean(1, keepdim=True) if kind == "layer" else 0.0
+        sd = torch.sqrt(((t - mean) ** 2).mean(1, keepdim=True) + EPS)
+        return (t - mean) / sd, sd
+
+    def through(d, k, th, sd):        # the gradient at a norm's input
+        d = d * s["gamma_" + k].double()
+        inner = th * (d * th).sum(1, keepdim=True) + (d.sum(1, keepdim=True) if c[k] == "layer" else 0.0)
+        return (d - inner / C) / sd
+
+    y = rows(s["y"])
+    v = y
+    if c["post"] != "none":
+        yh, ysd = normed(y, c["post"])
+        v = yh * s["gamma_post"].double() + s["beta_post"].double()
+    o = x + b * m * v
+    oh, osd = normed(o, c["pre"])
+    out = {"o": back(o), "u": back(oh * s["gamma_pre"].double() + s["beta_pre"].double())}
+    if not c["train"]:
+        return out
+    du = rows(s["du"])
+    do = rows(s["do"]) + through(du, "pre", oh, osd)
+    per = (do * v * m).reshape(N, H * W, C).sum(1)
+    dv = do * b * m
+    out["dx"], out["dgamma_pre"], out["dbeta_pre"] = back(do), (du * oh).sum(0), du.sum(0)
+    out["dscale"] = (per * s["gate"].double()).sum(0) if c["gate"] else per.sum(0)
+    out["dgate"] = per * a if c["gate"] else None
+    if c["post"] == "none":
+        out.update(dy=back(dv), dgamma_post=None, dbeta_post=None)
+    else:
+        out.update(dy=back(through(dv, "post", yh, ysd)), dgamma_post=(dv * yh).sum(0), dbeta_post=dv.sum(0))
+    return out
