@@ -255,8 +255,8 @@ def _run_own(s):
                     s["vu"], s["u"], s.get("stat"))
         if not c["train"]:
             return {"o": s["o"], "u": s["u"]}
-        dc.join_bwd(s["vdu"], s["du"], s["vdo"], s["do"], s["vy"], s["y"], s["vo"], s["o"], s["stat"], s["post"], s["scale"], s["gate"],
-                    s["drop"], s["pre"], s["vdx"], s["dx"], s["vdy"], s["dy"], s["grads"], 0, s["ws"])
+        dc.join_bwd(s["vdu"], s["du"], s["vdo"], s["do"], s["vy"], s["y"], s["vx"], s["x"], None, None, s["stat"], s["post"], s["scale"],
+                    s["gate"], s["drop"], s["pre"], s["vdx"], s["dx"], s["vdy"], s["dy"], s["grads"], 0, s["ws"])
         d = s["grads"]
         return {"o": s["o"], "u": s["u"], "dx": s["dx"], "dy": s["dy"], "dscale": d.scale, "dgate": d.gate, "dgamma_post": d.gamma_post,
                 "dbeta_post": d.beta_post, "dgamma_pre": d.gamma_pre, "dbeta_pre": d.beta_pre}
