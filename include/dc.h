@@ -411,6 +411,124 @@ dc_status dc_linear_bwd_filter(const dc_view* vx, const void* x, const dc_view* 
                                size_t workspace_bytes, void* stream);
 size_t dc_linear_bwd_filter_workspace_bytes(const dc_view* vx, const dc_view* vdy);
 
+/* ---- a gated residual block: the gated product, the join, dropout ---- */
+
+/*
+ * What such a block adds to the calls above:
+ *
+ *   u -> dc_gate_fwd -> h -> dc_linear_fwd -> y,   dc_join_fwd(y, x) -> o, and the next block's u
+ *
+ * and back: dc_join_bwd, then dc_gate_bwd_data through the second product, whose result is
+ * what dc_linear_bwd_data (act DC_ACT_NONE) and dc_linear_bwd_filter take for the first.
+ * Views, alignment, sizes and numbers as above; a view with H tokens of N sequences in rows
+ * of channels is W = 1, sc = 1, sh = C, sn = H C.
+ */
+
+/*
+ * Dropout whose mask is never stored: forward and backward passes form it again from these
+ * arguments, and the tiles of a decomposed image draw the mask of the whole one.
+ *
+ * A value is dropped with a chance of t / 65536, t the integer nearest 65536 p (ties to
+ * even, 65535 at most), and multiplied by 65536 / (65536 - t) if it stays; what is dropped is
+ * 0, whatever stood there.  0 <= p < 1.  Channels 8k .. 8k+7 of a pixel share the four words
+ * w0 .. w3 of Philox 4x32 with 10 rounds (Salmon, Moraes, Dror and Shaw, SC 2011) for the key
+ * `seed` and the counter whose lower 64 bits are the position
+ *   ((n ceil(C/8) + k) H + h) W + w       (sample n, row h, column w of the whole tensor)
+ * and whose upper 64 bits are offset + *step modulo 2^64: of the 16 bits that channel j of
+ * the eight takes, w[j/2]'s lower half for even j, its upper half for odd j, those below t
+ * drop it.  An offset of its own for each use (layer and training step) gives each a mask of
+ * its own.  step, in device memory (8-byte aligned) and read when the kernel runs, may be
+ * NULL (0): a captured graph's replays draw new masks as the program counts it up.
+ *
+ * The tensor lies in the whole one with its first sample, row and column at n0, h0, w0; H and
+ * W are the whole one's rows and columns, 0: as far as the tensor reaches.  P x Q (0: 1): the
+ * tensor holds the tiles of such a grid as consecutive samples, tile by tile, N / (P Q) of
+ * each, as DC_ALL_TILES tensors do; tile (p, q) starts at row h0 + p (view's H), column w0 +
+ * q (view's W).  Positions stay below 2^63 (DC_ERR_TOO_LARGE).
+ */
+typedef struct {
+    double p;
+    uint64_t seed, offset;
+    const uint64_t* step;
+    int32_t n0, h0, w0, H, W, P, Q;
+} dc_drop;
+
+/* y = x dropped out; with dy for x, its gradient.  y may be x (same view and type). */
+dc_status dc_dropout(const dc_drop* drop, const dc_view* vx, const void* x, const dc_view* vy, void* y, void* stream);
+
+/*
+ * Gated product over the channels of every pixel:
+ *   zg = Wg x + bg,  zu = Wu x + bu,  h = drop(act(zg) zu).
+ * w is [2K][C], Wg then Wu, of x's type; bias fp32 [2K], bg then bu, or NULL; drop NULL: none.
+ * zg and zu are written too unless both are NULL, for dc_gate_bwd_data: two tensors of one
+ * view (K channels), whole (fp32, bf16) or in 8 bits (DC_Q8).  K = vh->C; h is fp32 or bf16.
+ * Numbers are dc_linear_fwd's: the act DC_ACT_NONE takes zg itself.
+ */
+dc_status dc_gate_fwd(const dc_view* vx, const void* x, const void* w, const float* bias, int32_t act, const dc_drop* drop,
+                      const dc_view* vz, void* zg, void* zu, const dc_view* vh, void* h, void* stream);
+
+/*
+ * Gradient at its two sums from the gradient dy of the product after it:
+ *   dh = drop(W2^T dy),  dz = (dh zu act'(zg), then dh act(zg)),
+ * w is W2, [vdy->C][K] of dy's type, K = vz->C; dz has 2K channels, so that the first
+ * product's gradients are dc_linear_bwd_data's and dc_linear_bwd_filter's of w as a [2K][C]
+ * matrix.  h, drop(act(zg) zu) once more from what was kept, is written unless NULL.
+ */
+dc_status dc_gate_bwd_data(const dc_view* vdy, const void* dy, const void* w, int32_t act, const dc_drop* drop,
+                           const dc_view* vz, const void* zg, const void* zu, const dc_view* vh, void* h,
+                           const dc_view* vdz, void* dz, void* stream);
+
+/*
+ * A norm of a pixel x over its channels, in fp32: layer, (x - mean) r with r = (mean (x -
+ * mean)^2 + eps)^-1/2, or root mean square, x r with r = (mean x^2 + eps)^-1/2; times gamma,
+ * plus beta (fp32 [C] or NULL: 1 and 0).
+ */
+typedef enum { DC_NORM_NONE = 0, DC_NORM_LAYER = 1, DC_NORM_RMS = 2 } dc_norm_kind;
+typedef struct {
+    int32_t kind;
+    float eps;
+    const float *gamma, *beta;
+} dc_norm;
+
+/*
+ * Join of a block's branch y with the residual stream x:
+ *   o = x + scale gate drop(post(y)),  u = pre(o).
+ * post is the norm after the block, pre the one before the next block; NULL or DC_NORM_NONE:
+ * none (then u is NULL).  scale is fp32 [C], gate fp32 [N][C], one factor a sample and channel;
+ * either may be NULL (1).  x may be NULL (0).  u is formed from o before o's rounding.  stat
+ * [4][N][H][W] (mean and r of y, then of o; a mean of 0 for root mean square; untouched where
+ * there is no norm) is written unless NULL, and so is ckpt, o in 8 bits.  o may be x, u may
+ * be y (same view and type).
+ */
+dc_status dc_join_fwd(const dc_view* vy, const void* y, const dc_norm* post, const float* scale, const float* gate,
+                      const dc_drop* drop, const dc_view* vx, const void* x, const dc_norm* pre, const dc_view* vo, void* o,
+                      const dc_view* vu, void* u, float* stat, void* ckpt, void* stream);
+
+/*
+ * Its backward pass from du and d_o, the gradients at u and at o from elsewhere (either may be
+ * NULL, not both; without du the call goes as far as o, and pre, vx, x, vo, o are not looked at):
+ *   dO = d_o + (gradient of pre at o),  dx = dO,  dy = (gradient of post at y) of dO scale gate drop.
+ * With du, o is formed once more from y and x (NULL: 0), as the forward pass formed it; or, unless
+ * o is NULL, read as it was stored, in its type's precision, and x is not looked at.  y is needed
+ * where o is formed, where there is a post norm and where a gradient of scale or gate is wanted, else
+ * it may be NULL.  y, x and o may be in 8 bits (DC_Q8).  stat is what the forward pass wrote.  dx
+ * may be NULL.  grads (NULL: none): fp32, [C] each and [N][C] for gate; NULL where not wanted, and
+ * for parameters that the call does not have.  accumulate = 0 overwrites them, 1 adds to them.  dx
+ * may be d_o, dy may be y or du (same view and type).  workspace: at least
+ * dc_join_bwd_workspace_bytes(vdy, whether there is a gate) bytes, if there are grads.  The
+ * summation order is fixed.
+ */
+typedef struct {
+    float *scale, *gate, *gamma_post, *beta_post, *gamma_pre, *beta_pre;
+} dc_join_grads;
+dc_status dc_join_bwd(const dc_view* vdu, const void* du, const dc_view* vdo, const void* d_o, const dc_view* vy, const void* y,
+                      const dc_view* vx, const void* x, const dc_view* vo, const void* o, const float* stat,
+                      const dc_norm* post, const float* scale,
+                      const float* gate, const dc_drop* drop, const dc_norm* pre, const dc_view* vdx, void* dx,
+                      const dc_view* vdy, void* dy, const dc_join_grads* grads, int32_t accumulate, void* workspace,
+                      size_t workspace_bytes, void* stream);
+size_t dc_join_bwd_workspace_bytes(const dc_view* vdy, int32_t gate);
+
 #ifdef __cplusplus
 }
 #endif

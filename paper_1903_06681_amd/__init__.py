@@ -35,6 +35,8 @@ DC_BAND_NS, DC_BAND_WE, DC_BAND_CORNERS, DC_BAND_ALL = 1, 2, 4, 7
 DC_REGION_ALL, DC_REGION_INTERIOR, DC_REGION_BOUNDARY = 0, 1, 2
 DC_Q8 = 2   # view dtype: an activation checkpoint in 8 bits
 DC_ACT_NONE, DC_ACT_RELU, DC_ACT_GELU, DC_ACT_SILU = 0, 1, 2, 3
+DC_NORM_NONE, DC_NORM_LAYER, DC_NORM_RMS = 0, 1, 2
+NORM = {"none": DC_NORM_NONE, "layer": DC_NORM_LAYER, "rms": DC_NORM_RMS}
 ACT = {"none": DC_ACT_NONE, "relu": DC_ACT_RELU, "gelu": DC_ACT_GELU, "silu": DC_ACT_SILU}
 # capacity of the fixed workspace of dc_conv_bwd_filter_noalloc (include/dc.h)
 BWD_FILTER_NOALLOC_MAX_BYTES = 64 << 20
@@ -53,6 +55,7 @@ EXPORTS = (
     "dc_required_halo", "dc_halo_bands", "dc_tile_dims", "dc_status_string",
     "dc_ckpt_bytes", "dc_ckpt_save", "dc_ckpt_load", "dc_norm_fwd", "dc_norm_bwd", "dc_norm_bwd_workspace_bytes",
     "dc_linear_fwd", "dc_linear_bwd_data", "dc_linear_bwd_filter", "dc_linear_bwd_filter_workspace_bytes",
+    "dc_dropout", "dc_gate_fwd", "dc_gate_bwd_data", "dc_join_fwd", "dc_join_bwd", "dc_join_bwd_workspace_bytes",
 )
 
 
@@ -97,6 +100,42 @@ class View(ctypes.Structure):
     def q8(cls, N, C, H, W) -> "View":
         """Of the 8-bit checkpoint of such a tensor (a buffer of ckpt_bytes)."""
         return cls(N, C, H, W, 0, 0, 0, DC_Q8)
+
+
+class Drop(ctypes.Structure):
+    """``dc_drop``: a dropout whose mask is formed again wherever it is read.
+
+    p: the share that is dropped; seed and offset (an offset of its own for each use) choose
+    the mask; step: a CUDA int64 or uint64 tensor of one element that is added to the offset
+    when the kernel runs, or None.  n0, h0, w0, H, W, P, Q: where the tensor lies in the whole
+    one (a tile in its image; 0: the tensor is the whole).
+    """
+    _fields_ = ([("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)] +
+                [(n, ctypes.c_int32) for n in ("n0", "h0", "w0", "H", "W", "P", "Q")])
+
+    def __init__(self, p, seed, offset=0, step=None, n0=0, h0=0, w0=0, H=0, W=0, P=0, Q=0):
+        super().__init__(p, seed, offset, _ptr(step), n0, h0, w0, H, W, P, Q)
+        self._step = step                     # alive as long as its address is
+
+
+class Norm(ctypes.Structure):
+    """``dc_norm``: a norm over a pixel's channels; gamma and beta are fp32 tensors or None."""
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("_gamma", ctypes.c_void_p), ("_beta", ctypes.c_void_p)]
+
+    def __init__(self, kind, eps, gamma=None, beta=None):
+        super().__init__(kind, eps, _ptr(gamma), _ptr(beta))
+        self.gamma, self.beta = gamma, beta
+
+
+class JoinGrads(ctypes.Structure):
+    """``dc_join_grads``: where join_bwd writes the parameters' gradients (fp32 tensors or None)."""
+    _names = ("scale", "gate", "gamma_post", "beta_post", "gamma_pre", "beta_pre")
+    _fields_ = [("_" + n, ctypes.c_void_p) for n in _names]
+
+    def __init__(self, scale=None, gate=None, gamma_post=None, beta_post=None, gamma_pre=None, beta_pre=None):
+        t = (scale, gate, gamma_post, beta_post, gamma_pre, beta_pre)
+        super().__init__(*map(_ptr, t))
+        self.scale, self.gate, self.gamma_post, self.beta_post, self.gamma_pre, self.beta_pre = t
 
 
 class DcError(RuntimeError):
@@ -148,8 +187,16 @@ _lib.dc_linear_bwd_data.argtypes = [_W, _V, _V, _I, _W, _V, _W, _V, _W, _V, _V]
 _lib.dc_linear_bwd_filter.argtypes = [_W, _V, _W, _V, _V, _V, _I, _V, _Z, _V]
 _lib.dc_linear_bwd_filter_workspace_bytes.argtypes = [_W, _W]
 _lib.dc_linear_bwd_filter_workspace_bytes.restype = _Z
+_D, _N, _G = ctypes.POINTER(Drop), ctypes.POINTER(Norm), ctypes.POINTER(JoinGrads)
+_lib.dc_dropout.argtypes = [_D, _W, _V, _W, _V, _V]
+_lib.dc_gate_fwd.argtypes = [_W, _V, _V, _V, _I, _D, _W, _V, _V, _W, _V, _V]
+_lib.dc_gate_bwd_data.argtypes = [_W, _V, _V, _I, _D, _W, _V, _V, _W, _V, _W, _V, _V]
+_lib.dc_join_fwd.argtypes = [_W, _V, _N, _V, _V, _D, _W, _V, _N, _W, _V, _W, _V, _V, _V, _V]
+_lib.dc_join_bwd.argtypes = [_W, _V, _W, _V, _W, _V, _W, _V, _W, _V, _V, _N, _V, _V, _D, _N, _W, _V, _W, _V, _G, _I, _V, _Z, _V]
+_lib.dc_join_bwd_workspace_bytes.argtypes = [_W, _I]
+_lib.dc_join_bwd_workspace_bytes.restype = _Z
 for _n in ("dc_ckpt_save", "dc_ckpt_load", "dc_norm_fwd", "dc_norm_bwd", "dc_linear_fwd", "dc_linear_bwd_data",
-           "dc_linear_bwd_filter"):
+           "dc_linear_bwd_filter", "dc_dropout", "dc_gate_fwd", "dc_gate_bwd_data", "dc_join_fwd", "dc_join_bwd"):
     getattr(_lib, _n).restype = ctypes.c_int32
 for _n in ("dc_conv_fwd", "dc_conv_bwd_data", "dc_conv_bwd_filter", "dc_conv_bwd_filter_noalloc",
            "dc_halo_pack", "dc_halo_unpack", "dc_halo_pack_bands", "dc_halo_unpack_bands",
@@ -375,3 +422,47 @@ def linear_bwd_filter(vx, x, vdy, dy, dw, db, accumulate, workspace, stream=None
     """dw (=|+=) sum over pixels of dy x^T, db (=|+=) sum over pixels of dy (or None)."""
     _check(_lib.dc_linear_bwd_filter(_view(vx), _ptr(x), _view(vdy), _ptr(dy), _ptr(dw), _ptr(db), accumulate,
                                      _ptr(workspace), _bytes(workspace), _stream(stream)), "dc_linear_bwd_filter")
+
+
+# ------------------------------------- a gated residual block
+
+def dropout(drop, vx, x, vy, y, stream=None):
+    """y <- x dropped out (drop: Drop); the same call on dy is its gradient."""
+    _check(_lib.dc_dropout(_view(drop), _view(vx), _ptr(x), _view(vy), _ptr(y), _stream(stream)), "dc_dropout")
+
+
+def gate_fwd(vx, x, w, bias, act, drop, vz, zg, zu, vh, h, stream=None):
+    """h <- drop(act(zg) zu), zg and zu the products of x with w's first and second half; bias,
+    drop, and zg with zu (whole or 8-bit, kept for gate_bwd_data) may be None."""
+    _check(_lib.dc_gate_fwd(_view(vx), _ptr(x), _ptr(w), _ptr(bias), act, _view(drop), _view(vz), _ptr(zg), _ptr(zu),
+                            _view(vh), _ptr(h), _stream(stream)), "dc_gate_fwd")
+
+
+def gate_bwd_data(vdy, dy, w, act, drop, vz, zg, zu, vh, h, vdz, dz, stream=None):
+    """dz <- gradient at zg and zu (2 K channels) from dy, the gradient of the product w after the
+    gated one; h <- drop(act(zg) zu) again unless None."""
+    _check(_lib.dc_gate_bwd_data(_view(vdy), _ptr(dy), _ptr(w), act, _view(drop), _view(vz), _ptr(zg), _ptr(zu),
+                                 _view(vh), _ptr(h), _view(vdz), _ptr(dz), _stream(stream)), "dc_gate_bwd_data")
+
+
+def join_fwd(vy, y, post, scale, gate, drop, vx, x, pre, vo, o, vu, u, stat=None, ckpt=None, stream=None):
+    """o <- x + scale gate drop(post(y)), u <- pre(o) (post, pre: Norm or None); stat [4][N][H][W]
+    and ckpt (o in 8 bits) for the backward pass."""
+    _check(_lib.dc_join_fwd(_view(vy), _ptr(y), _view(post), _ptr(scale), _ptr(gate), _view(drop), _view(vx), _ptr(x),
+                            _view(pre), _view(vo), _ptr(o), _view(vu), _ptr(u), _ptr(stat), _ptr(ckpt), _stream(stream)),
+           "dc_join_fwd")
+
+
+def join_bwd_workspace_bytes(vdy, gate):
+    return _lib.dc_join_bwd_workspace_bytes(ctypes.byref(vdy), int(bool(gate)))
+
+
+def join_bwd(vdu, du, vdo, do, vy, y, vx, x, vo, o, stat, post, scale, gate, drop, pre, vdx, dx, vdy, dy, grads,
+             accumulate, workspace, stream=None):
+    """dx, dy <- gradients of join_fwd at x and y from those at u and o; grads (JoinGrads or None)
+    (=|+=) the parameters'.  o is formed again from y and x, or read where it is given; the three
+    are whole or their 8-bit forms."""
+    _check(_lib.dc_join_bwd(_view(vdu), _ptr(du), _view(vdo), _ptr(do), _view(vy), _ptr(y), _view(vx), _ptr(x),
+                            _view(vo), _ptr(o), _ptr(stat), _view(post), _ptr(scale), _ptr(gate), _view(drop), _view(pre), _view(vdx),
+                            _ptr(dx), _view(vdy), _ptr(dy), _view(grads), accumulate, _ptr(workspace),
+                            _bytes(workspace), _stream(stream)), "dc_join_bwd")

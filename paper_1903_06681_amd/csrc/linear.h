@@ -94,7 +94,7 @@ __device__ __forceinline__ Chunk chunk_of(const Slots& s, int ci) {
     return c;
 }
 
-enum { WEIGHT, PIXEL, LONG };   // which way an operand is found: see Stage
+enum { WEIGHT, PIXEL, LONG, PAIR };   // which way an operand is found: see Stage
 
 static constexpr int kRow = 128;   // bytes of k a slice
 
@@ -114,6 +114,8 @@ struct Shape {
 //   WEIGHT  a matrix, rows [row][k] (RK) or [k][row] (KR)
 //   PIXEL   rows are slots: k the channels' planes (KR), or contiguous (RK: rows of channels)
 //   LONG    k runs over the slots, rows are channels: planes (RK), or rows of channels (KR)
+//   PAIR    two matrices of o.rows rows, one below the other (RK): of the block's rows,
+//           groups of 32 are taken from the one and the other in turn
 // A thread's chunks of 16 bytes follow each other in LDS at a distance of the
 // workgroup; which chunk of memory they hold is permuted, so that LDS is written in
 // order (as direct loads must) and read without bank conflicts.
@@ -145,7 +147,11 @@ struct Stage {
         c = (threadIdx.x % CPR) ^ mix(r0);
         left = E;
         bool in = true;
-        if constexpr (SRC == WEIGHT && KIND == RK) {
+        if constexpr (SRC == PAIR) {               // first: of the pair
+            static_assert(KIND == RK && (STEP <= 32 || STEP == 64));
+            at[0] = int64_t(first + r0 % 32 + (r0 / 32 ? o.rows : 0)) * o.ld + c * E;
+            left = o.rows - (first + r0 % 32);
+        } else if constexpr (SRC == WEIGHT && KIND == RK) {
             at[0] = int64_t(first + r0) * o.ld + c * E;
             left = o.rows - (first + r0);          // rows from this one on
         } else if constexpr (SRC == WEIGHT) {
@@ -169,8 +175,15 @@ struct Stage {
             at[0] = first + c * E;
             left = o.rows - (first + c * E);
         }
-        whole = __all(in && left > (KIND == RK && SRC != PIXEL ? (U - 1) * STEP : 0));
+        whole = __all(in && left > (SRC == PAIR ? pair_row(U - 1) : KIND == RK && SRC != PIXEL ? (U - 1) * STEP : 0));
     }
+
+    // PAIR: row of chunk i after chunk 0's; whether it is one of the second matrix (of the other, where
+    // a thread's chunks lie 64 rows apart)
+    __device__ __forceinline__ static constexpr int pair_row(int i) {
+        return STEP == 64 ? i * 32 : (i * STEP / 32) / 2 * 32 + i * STEP % 32;
+    }
+    __device__ __forceinline__ static constexpr bool pair_second(int i) { return STEP < 64 && (i * STEP / 32) % 2; }
 
     // f(i, element, elements of the chunk that count) for the chunks of the slice at k0
     template <typename F>
@@ -191,6 +204,8 @@ struct Stage {
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 if constexpr (SRC == PIXEL) f(i, at[i] + k0, at[i] >= 0 ? n : 0);
+                else if constexpr (SRC == PAIR)
+                    f(i, at[0] + k0 + (pair_row(i) + (pair_second(i) ? int64_t(o.rows) : 0)) * o.ld, left - pair_row(i) > 0 ? n : 0);
                 else f(i, at[0] + k0 + i * STEP * o.ld, left - i * STEP > 0 ? n : 0);
             }
         } else {

@@ -9,85 +9,19 @@
 // loop's 32 slices one after the other 16 us.
 #include <algorithm>
 
-#include "linear_pass.h"
+#include "linear_few.h"
 
 namespace dc {
-
-static constexpr int kFewWaves = 16;
-typedef float f32x4_acc __attribute__((ext_vector_type(4)));
-
-template <typename T>
-__device__ __forceinline__ void multiply16(f32x4_acc& acc, const uint4& a, const uint4& b) {
-    if constexpr (sizeof(T) == 2) {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0,
-                                                      0, 0);
-    } else {
-        const f32x4_t fa = __builtin_bit_cast(f32x4_t, a), fb = __builtin_bit_cast(f32x4_t, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fb[i], acc, 0, 0, 0);
-    }
-}
 
 // NT: tiles of 16 pixels.  BWD: weights [k][row], and the activation's slope.
 template <typename T, bool BWD, bool CL, int NT>
 __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a, int M) {
-    constexpr int E = 16 / int(sizeof(T)), STEP = 4 * E;      // k of a lane's chunk, of a wave's step
     __shared__ float sums[kFewWaves][NT * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int o0 = blockIdx.x * 16, m0 = blockIdx.y * NT * 16, red = a.a.red;
+    const int o0 = blockIdx.x * 16, m0 = blockIdx.y * NT * 16;
     const int hw = int(a.s.dsample.d) / a.s.cpr * a.s.len;
-    auto offset = [&](int m, const auto& v) __attribute__((always_inline)) {   // of channel 0 of pixel m
-        const int n = m / hw, pix = m - n * hw, r = pix / a.s.len;
-        return n * v.sn + r * v.sh + (pix - r * a.s.len);
-    };
-    const T* w = reinterpret_cast<const T*>(a.a.p);
-    const T* x = reinterpret_cast<const T*>(a.b.p);
     const int row = min(o0 + (lane & 15), a.rows - 1);
-    int64_t xo[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) xo[t] = offset(min(m0 + t * 16 + (lane & 15), M - 1), a.b);
-    // eight (four) values of k of which n count, `step` elements apart; past the end the last one's address
-    auto gather = [&](const T* p, int64_t step, int n) __attribute__((always_inline)) {
-        T e[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const T f = p[max(min(i, n - 1), 0) * step];
-            e[i] = i < n ? f : T(0);
-        }
-        uint4 r;
-        __builtin_memcpy(&r, e, 16);
-        return r;
-    };
-    // this wave's steps of k
-    const int steps = (red + STEP - 1) / STEP, per = (steps + kFewWaves - 1) / kFewWaves;
-    const int s1 = min((wave + 1) * per, steps);
-    f32x4_acc acc[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f32x4_acc{0, 0, 0, 0};
-#pragma unroll 4
-    for (int s = wave * per; s < s1; ++s) {
-        const int k = s * STEP + (lane >> 4) * E, n = red - k, kk = min(k, red - 1);
-        uint4 fa = make_uint4(0, 0, 0, 0), fb[NT];
-        if constexpr (BWD) fa = gather(w + int64_t(kk) * a.a.ld + row, a.a.ld, n);
-        else if (n > 0) fa = keep16<T>(load16(w, row * a.a.ld + k, a.a.end), n);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            fb[t] = make_uint4(0, 0, 0, 0);
-            if constexpr (CL) {
-                if (n > 0) fb[t] = keep16<T>(load16(x, xo[t] + k, a.b.end), n);
-            } else {
-                fb[t] = gather(x + xo[t] + kk * a.b.sc, a.b.sc, n);
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) multiply16<T>(acc[t], fa, fb[t]);
-    }
-    // lane: pixel lane % 16, channels 4 (lane / 16) .. + 3
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sums[wave][t * 256 + (4 * (lane >> 4) + r) * 16 + (lane & 15)] = acc[t][r];
-    __syncthreads();
+    few_sums<T, BWD, CL, NT>(sums, a, row, m0, M, hw, lane, wave);
     // channels next to each other in memory (rows of channels) lie next to each other on the lanes
     for (int e = threadIdx.x; e < NT * 256; e += 64 * kFewWaves) {
         const int in = e & 255, o = o0 + (CL ? in & 15 : in >> 4), mt = CL ? in >> 4 : in & 15, m = m0 + (e >> 8) * 16 + mt;
@@ -97,12 +31,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
 #pragma unroll
         for (int i = 0; i < kFewWaves; ++i) v[0] += sums[i][at];
         auto put = [&](const View& t, float f) __attribute__((always_inline)) {
-            const int64_t k = offset(m, t) + o * t.sc;
+            const int64_t k = few_offset(a.s, hw, m, t) + o * t.sc;
             if (t.dt == DC_F32) store1(reinterpret_cast<float*>(t.p) + k, f);
             else store1(reinterpret_cast<__bf16*>(t.p) + k, f);
         };
         auto get = [&](const View& t) __attribute__((always_inline)) {
-            const int64_t k = offset(m, t) + o * t.sc;
+            const int64_t k = few_offset(a.s, hw, m, t) + o * t.sc;
             return t.dt == DC_F32 ? load1(reinterpret_cast<const float*>(t.p) + k) : load1(reinterpret_cast<const __bf16*>(t.p) + k);
         };
         if constexpr (BWD) {
@@ -129,10 +63,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
     }
 }
 
-static int pixels_in(const LinearArgs& a) {
-    return a.s.chunks / int(a.s.dsample.d) * (int(a.s.dsample.d) / a.s.cpr * a.s.len);
-}
-
 // Up to 64 pixels, or a long sum with few blocks of the tile loop to share it.  Forward
 // where the loop's slices are dear (fp32's matrix rate, operands staged through registers):
 // up to 64 blocks, a workgroup a compute unit here.  fp32, 1024 channels to 256 on 32 x 32
@@ -141,7 +71,7 @@ static int pixels_in(const LinearArgs& a) {
 // 16.4 and 13.0.  z in 8 bits is written 32 channels at a time: the tile loop's.
 bool linear_few(const LinearArgs& a, bool bwd, bool f32) {
     if (!bwd && a.z.dt == DC_Q8) return false;
-    const int64_t M = pixels_in(a);
+    const int64_t M = few_pixels(a);
     const int limit = !bwd && (f32 || !a.direct) ? 64 : 31;
     return M <= 64 || (a.a.red >= 256 && (a.rows + 63) / 64 * ((M + 63) / 64) <= limit);
 }
@@ -160,7 +90,7 @@ static void launch(const LinearArgs& a, int M, hipStream_t s) {
 }
 
 hipError_t launch_linear_few(const LinearArgs& a, bool bwd, bool f32, hipStream_t s) {
-    const int M = pixels_in(a);
+    const int M = few_pixels(a);
     if (f32) bwd ? launch<float, true>(a, M, s) : launch<float, false>(a, M, s);
     else bwd ? launch<__bf16, true>(a, M, s) : launch<__bf16, false>(a, M, s);
     return hipGetLastError();

@@ -12,8 +12,9 @@ static constexpr int kNormWaves = 8;    // most waves of a workgroup
 struct NormLane {
     int px, unit, ng, pg, wave;
 };
-template <int LPX>
-__device__ __forceinline__ NormLane norm_lane(const NormArgs& a) {
+// A: the arguments of the norm, or of the join of a branch (join.h)
+template <int LPX, typename A>
+__device__ __forceinline__ NormLane norm_lane(const A& a) {
     const int lane = threadIdx.x & 63;
     NormLane l;
     l.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -26,8 +27,8 @@ __device__ __forceinline__ NormLane norm_lane(const NormArgs& a) {
 
 // Sums of K values over the units of a pixel, in all of them.  Fixed order: the
 // lanes of the wave that share the pixel, then the waves.
-template <int LPX, int K>
-__device__ __forceinline__ void pixel_sum(float (&v)[K], const NormArgs& a, const NormLane& l,
+template <int LPX, int K, typename A>
+__device__ __forceinline__ void pixel_sum(float (&v)[K], const A& a, const NormLane& l,
                                           float (&red)[K][kNormWaves * LPX]) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
@@ -101,8 +102,8 @@ __device__ __forceinline__ void store_any(const View& t, const Pixel& p, int c0,
 
 // f(slot, block) for the blocks of a unit: R of them held in registers, or (R = 0)
 // any number, one after the other in slot 0
-template <int R, typename F>
-__device__ __forceinline__ void each_block(const NormArgs& a, const NormLane& l, F&& f) {
+template <int R, typename A, typename F>
+__device__ __forceinline__ void each_block(const A& a, const NormLane& l, F&& f) {
     if constexpr (R) {
 #pragma unroll
         for (int i = 0; i < R; ++i)
@@ -110,6 +111,29 @@ __device__ __forceinline__ void each_block(const NormArgs& a, const NormLane& l,
     } else {
         for (int cb = l.unit; cb < a.blocks; cb += l.ng) f(0, cb);
     }
+}
+
+// Sums of V values over the LPX pixel lanes of a wave, by halving: each step a lane gives away
+// half of its values.  Lane px ends with those of values px * V / LPX + e, in v[e]; where
+// there are fewer values than lanes, neighbours hold the same one.
+template <int D, int N, int V>
+__device__ __forceinline__ void sum_step(float (&v)[V], int lane) {
+    if constexpr (D >= 1 && N >= 1) {
+        const bool hi = lane & D;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float keep = hi ? v[k + N] : v[k], give = hi ? v[k] : v[k + N];
+            v[k] = keep + __shfl_xor(give, D);
+        }
+        sum_step<D / 2, N / 2>(v, lane);
+    } else if constexpr (D >= 1) {
+        v[0] += __shfl_xor(v[0], D);
+        sum_step<D / 2, N>(v, lane);
+    }
+}
+template <int LPX, int V>
+__device__ __forceinline__ void sum_lanes(float (&v)[V], int lane) {
+    sum_step<LPX / 2, V / 2>(v, lane);
 }
 
 // Launch K<type, LPX, R, CL> as planned (norm_plan keeps to these).  HELD16: blocks that a

@@ -19,21 +19,6 @@
 
 namespace dc {
 
-// Sums of 64 values over the LPX pixel lanes of a wave: lane px ends with those of
-// values px * (64 / LPX) + e, in v[e].
-template <int LPX, int D = LPX / 2, int N = 32>
-__device__ __forceinline__ void sum_lanes(float (&v)[64], int lane) {
-    if constexpr (D >= 1) {
-        const bool hi = lane & D;
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const float keep = hi ? v[k + N] : v[k], give = hi ? v[k] : v[k + N];
-            v[k] = keep + __shfl_xor(give, D);
-        }
-        sum_lanes<LPX, D / 2, N / 2>(v, lane);
-    }
-}
-
 // XT: float or __bf16 of the tile, or char: the checkpoint.
 template <typename XT, typename DT, int LPX, int R, bool CL>
 __global__ __launch_bounds__(512, LPX == 64 && R == 1 ? 3 : 2) void norm_bwd_kernel(NormArgs a) {
