@@ -11,6 +11,7 @@ namespace dc {
 // The draw of a tensor [N][C][H][W]; no drop: t = 0.
 static dc_status drop_args(const dc_drop* d, const dc_view& v, int32_t C, DropArgs* a) {
     std::memset(a, 0, sizeof(*a));
+    a->scale = 1.0f;
     if (!d) return DC_OK;
     if (!(d->p >= 0 && d->p < 1)) return DC_ERR_ARG;
     if (d->n0 < 0 || d->h0 < 0 || d->w0 < 0 || d->H < 0 || d->W < 0 || d->P < 0 || d->Q < 0) return DC_ERR_ARG;
@@ -262,8 +263,8 @@ dc_status dc_join_bwd(const dc_view* vdu, const void* du, const dc_view* vdo, co
     a.du = device_view(vdu, du);
     a.dr = device_view(vdo, d_o);
     a.y = device_view(need_y ? vy : nullptr, y);
-    a.o = device_view(du ? vo : nullptr, o);
-    a.x = device_view(form_o ? vx : nullptr, x);
+    a.form_o = form_o;
+    a.x = form_o ? device_view(vx, x) : device_view(du ? vo : nullptr, o);
     a.dx = device_view(vdx, dx);
     a.dy = device_view(vdy, dy);
     a.qm = map_of(*vdy, vdy->C);

@@ -10,7 +10,8 @@
 
 namespace dc {
 
-template <int LPX, int R, bool CL>
+// Planes: as in the layer norm (norm.h) a lane holds one pixel's blocks of 32 channels.
+template <int LPX, int R>
 __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
     constexpr int H = R ? R : 1;
     __shared__ float red[4][1][kNormWaves * LPX];
@@ -24,16 +25,16 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
     uint32_t wx[H][32];
     auto load_y = [&](int i, int cb) __attribute__((always_inline)) {
         uint32_t w[32];
-        load_raw<CL>(w, a.y, a.qm, p, cb * 32, a.C);
-        raw_values<CL>(v[i], w, a.y, cb * 32, a.C);
+        load_raw<false>(w, a.y, a.qm, p, cb * 32, a.C);
+        raw_values<false>(v[i], w, a.y, cb * 32, a.C);
     };
     if constexpr (R) {
         uint32_t wy[H][32];
         each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
-            load_raw<CL>(wy[i], a.y, a.qm, p, cb * 32, a.C);
-            if (a.x.p) load_raw<CL>(wx[i], a.x, a.qm, p, cb * 32, a.C);
+            load_raw<false>(wy[i], a.y, a.qm, p, cb * 32, a.C);
+            if (a.x.p) load_raw<false>(wx[i], a.x, a.qm, p, cb * 32, a.C);
         });
-        each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) { raw_values<CL>(v[i], wy[i], a.y, cb * 32, a.C); });
+        each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) { raw_values<false>(v[i], wy[i], a.y, cb * 32, a.C); });
     }
     // mean and 1 / deviation of what `form` leaves in v
     auto moments = [&](const JoinNorm& k, int at, float& mu, float& r, auto&& form) __attribute__((always_inline)) {
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
         const int c0 = cb * 32;
         if constexpr (!R) {
             load_y(0, cb);
-            if (a.x.p) load_raw<CL>(wx[0], a.x, a.qm, p, c0, a.C);
+            if (a.x.p) load_raw<false>(wx[0], a.x, a.qm, p, c0, a.C);
         }
         if (a.post.kind) {
             float g[32], b[32];
@@ -90,24 +91,17 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
         if (a.drop.t) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const Philox w = philox(dp.pos + uint64_t(cb * 4 + k) * uint64_t(a.drop.plane), dp.ctr, a.drop.seed);
+                float keep[8];
+                keep8(keep, a.drop, dp, cb * 4 + k);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    v[i][8 * k + j] = kept(w, j, a.drop.t) ? v[i][8 * k + j] * a.drop.scale : 0.0f;
+                for (int j = 0; j < 8; ++j) v[i][8 * k + j] = dropped(v[i][8 * k + j], keep[j]);
             }
         }
-        if (a.scale || a.gate) {
-            float f[32];
-            load_factor<LPX>(f, a, p, c0);
+        float f[32], x[32];
+        load_factor<LPX>(f, a, p, c0);
+        if (a.x.p) raw_values<false>(x, wx[i], a.x, c0, a.C);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[i][j] *= f[j];
-        }
-        if (a.x.p) {
-            float x[32];
-            raw_values<CL>(x, wx[i], a.x, c0, a.C);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[i][j] += x[j];
-        }
+        for (int j = 0; j < 32; ++j) v[i][j] = fmaf(v[i][j], f[j], a.x.p ? x[j] : 0.0f);
         if (c0 + 32 > a.C) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[i][j] = c0 + j < a.C ? v[i][j] : 0.0f;
@@ -123,7 +117,7 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
     each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
         const int c0 = cb * 32;
         if constexpr (!R) join(0, cb);
-        store_any<CL>(a.o, p, c0, a.C, v[i]);
+        store_any<false>(a.o, p, c0, a.C, v[i]);
         if (a.q) q8_store_block(a.q, a.qm, p, cb, v[i]);
         if (a.pre.kind && a.u.p) {
             float g[32], b[32];
@@ -131,27 +125,161 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
             load_params<LPX>(b, a.pre.beta, c0, a.C, 0.0f);
 #pragma unroll
             for (int j = 0; j < 32; ++j) g[j] = fmaf(g[j], (v[i][j] - mu2) * r2, b[j]);
-            store_any<CL>(a.u, p, c0, a.C, g);
+            store_any<false>(a.u, p, c0, a.C, g);
         }
     });
 }
 
-// As the layer norm's (norm_fwd.hip): rows of channels with a pixel's lanes next to each
-// other, tiles with 64 pixels a wave, or 16 where there are few or many channels.
+// Rows of channels: eight channels a lane, a row's lanes next to each other.
+template <int LPX, int R>
+__global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
+    constexpr int H = R ? R : 1;
+    __shared__ float red[4][1][kJoinWaves * LPX];
+    const JoinLane l = join_lane<LPX, true>(a);
+    const int wg = int(blockIdx.y * gridDim.x + blockIdx.x);
+    if (wg >= a.grid) return;
+    const int m = (wg * a.pg + l.pg) * LPX + l.px;
+    const bool in = m < a.px.M;
+    const Pixel p = pixel_of(a.px, m);
+    float v[H][8];
+    u32x8 wx[H];
+    auto load_y = [&](int i, int e) __attribute__((always_inline)) {
+        values8<true>(v[i], load8<true>(a.y, a.qm, p, 8 * e, a.C), a.y, 8 * e, a.C);
+    };
+    if constexpr (R) {
+        u32x8 wy[H];
+        each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) {
+            wy[i] = load8<true>(a.y, a.qm, p, 8 * e, a.C);
+            if (a.x.p) wx[i] = load8<true>(a.x, a.qm, p, 8 * e, a.C);
+        });
+        each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) { values8<true>(v[i], wy[i], a.y, 8 * e, a.C); });
+    }
+    // mean and 1 / deviation of what `form` leaves in v
+    auto moments = [&](const JoinNorm& k, int at, float& mu, float& r, auto&& form) __attribute__((always_inline)) {
+        float s[1] = {0};
+        mu = 0;
+        if (k.kind == DC_NORM_LAYER) {
+            each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) {
+                if constexpr (!R) form(i, e);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[0] += v[i][j];
+            });
+            lane_sum<LPX, true>(s, a, l, red[at]);
+            mu = s[0] * a.invC;
+            s[0] = 0;
+        }
+        each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) {
+            if constexpr (!R) form(i, e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = 8 * e + j < a.C ? v[i][j] - mu : 0.0f;
+                s[0] = fmaf(d, d, s[0]);
+            }
+        });
+        lane_sum<LPX, true>(s, a, l, red[at + 1]);
+        r = 1.0f / sqrtf(s[0] * a.invC + k.eps);
+        if (a.stat && in && l.unit == 0) {
+            a.stat[int64_t(at) * a.px.M + m] = mu;
+            a.stat[int64_t(at + 1) * a.px.M + m] = r;
+        }
+    };
+    float mu1 = 0, r1 = 0;
+    if (a.post.kind) moments(a.post, 0, mu1, r1, load_y);
+    DropPixel dp{};
+    if (a.drop.t) dp = drop_pixel(a.drop, p.n, p.pix);
+    // y in v -> o
+    auto join = [&](int i, int e) __attribute__((always_inline)) {
+        const int c0 = 8 * e;
+        if constexpr (!R) {
+            load_y(0, e);
+            if (a.x.p) wx[0] = load8<true>(a.x, a.qm, p, c0, a.C);
+        }
+        if (a.post.kind) {
+            float g[8], b[8];
+            params8<false>(g, a.post.gamma, c0, a.C, 1.0f);
+            params8<false>(b, a.post.beta, c0, a.C, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = fmaf(g[j], (v[i][j] - mu1) * r1, b[j]);
+        }
+        float f[8], k[8], x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        keep8(k, a.drop, dp, e);
+        factor8<false>(f, a, p, c0);
+        if (a.x.p) values8<true>(x, wx[i], a.x, c0, a.C);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = fmaf(dropped(v[i][j], k[j]), f[j], x[j]);
+        clear8(v[i], c0, a.C);
+    };
+    if constexpr (R) each_eight<R>(a, l, join);
+    float mu2 = 0, r2 = 0;
+    if (a.pre.kind) moments(a.pre, 2, mu2, r2, join);
+    // the four lanes of a block of 32 channels stay together: its scale is theirs
+    each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) {
+        const int c0 = 8 * e;
+        if constexpr (!R) join(0, e);
+        if (in) store8<true>(a.o, p, c0, a.C, v[i]);
+        if (a.q) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = max(top, abs_bits(v[i][j]));
+            // lanes past the last eight hold nothing and are not here: they read as 0 or as themselves
+#pragma unroll
+            for (int d = 1; d < 4; d *= 2) {
+                const uint32_t other = __shfl_xor(top, d);
+                top = max(top, (e ^ d) * 8 < a.C ? other : 0u);
+            }
+            const uint32_t s = q8_scale(top);
+            const float per = q8_per(s);
+            const int64_t at = int64_t(c0 / 32) * a.qm.HW + p.pix;
+            if (in) {
+                uint2* d = reinterpret_cast<uint2*>(a.q + p.n * a.qm.qn + at * 32 + c0 % 32);
+                *d = make_uint2(q8_pack(v[i][0], v[i][1], v[i][2], v[i][3], per), q8_pack(v[i][4], v[i][5], v[i][6], v[i][7], per));
+                if (e % 4 == 0) reinterpret_cast<uint8_t*>(a.q)[a.qm.s0 + p.n * a.qm.sn + at] = uint8_t(s);
+                if (c0 + 8 >= a.C)      // the block's channels past the last lane's
+                    for (int k = e % 4 + 1; k < 4; ++k) d[k - e % 4] = make_uint2(0, 0);
+            }
+        }
+        if (a.pre.kind && a.u.p) {
+            float g[8], b[8];
+            params8<false>(g, a.pre.gamma, c0, a.C, 1.0f);
+            params8<false>(b, a.pre.beta, c0, a.C, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = fmaf(g[j], (v[i][j] - mu2) * r2, b[j]);
+            if (in) store8<true>(a.u, p, c0, a.C, g);
+        }
+    });
+}
+
+// Planes, forward: as the layer norm's (norm_fwd.hip), 32 channels a lane, 64 pixels a wave, or
+// 16 where there are few or many channels.  The others: eight channels a lane.  Rows: as many
+// lanes as a row has eights, up to 64, then up to eight waves, then two eights a lane.
+// Planes, backward: 64 pixels a wave, fewer where there are few, or more channels than eight
+// waves hold.
 void join_plan(JoinArgs& a, bool backward) {
     a.blocks = (a.C + 31) / 32;
     a.invC = 1.0f / float(a.C);
-    const int64_t waves = (int64_t(a.px.M) + 63) / 64 * a.blocks;
-    if (a.cl)
-        a.lpx = a.blocks >= 16 ? 4 : 16;
-    else
-        a.lpx = a.blocks <= (backward ? 1 : 2) * kNormWaves && waves >= 2048 ? 64 : 16;
-    const int sb = 64 / a.lpx;
-    a.nw = std::min((a.blocks + sb - 1) / sb, kNormWaves);
-    const int held = (a.blocks + a.nw * sb - 1) / (a.nw * sb);
-    a.held = held <= 1 ? 1 : held == 2 && a.lpx == 64 ? 2 : 0;
+    const int eights = (a.C + 7) / 8;
+    const int64_t M = a.px.M, waves = (M + 63) / 64 * a.blocks;
+    if (a.cl) {
+        int u = 4;
+        while (u < eights && u < 64) u *= 2;
+        a.lpx = 64 / u;
+        a.held = eights <= 8 * u ? 1 : eights <= 16 * u ? 2 : 0;
+        a.nw = std::min((eights + u * std::max(a.held, 1) - 1) / (u * std::max(a.held, 1)), kJoinWaves);
+    } else if (backward) {
+        a.lpx = eights <= 16 && waves >= 1024 ? 64 : eights <= 64 ? 16 : 4;
+        if (eights > 256) a.lpx = 16;
+        const int u = 64 / a.lpx;
+        a.held = eights <= 8 * u ? 1 : eights <= 16 * u ? 2 : 0;
+        a.nw = std::min((eights + u * std::max(a.held, 1) - 1) / (u * std::max(a.held, 1)), kJoinWaves);
+    } else {
+        a.lpx = a.blocks <= 2 * kNormWaves && waves >= 2048 ? 64 : 16;
+        const int sb = 64 / a.lpx;
+        a.nw = std::min((a.blocks + sb - 1) / sb, kNormWaves);
+        const int held = (a.blocks + a.nw * sb - 1) / (a.nw * sb);
+        a.held = held <= 1 ? 1 : held == 2 && a.lpx == 64 ? 2 : 0;
+    }
     if (!backward) {
-        a.groups = int((int64_t(a.px.M) + a.lpx - 1) / a.lpx);
+        a.groups = int((M + a.lpx - 1) / a.lpx);
         a.pg = std::max(1, std::min(4 / a.nw, a.groups / 512));
         a.grid = (a.groups + a.pg - 1) / a.pg;
         return;
@@ -160,19 +288,18 @@ void join_plan(JoinArgs& a, bool backward) {
     a.samples = a.gate ? a.px.M / a.px.HW : 1;
     a.span = a.gate ? a.px.HW : a.px.M;
     a.groups = int((int64_t(a.span) + a.lpx - 1) / a.lpx);
+    // Units: slices of a sample's groups.  Workgroups take them in turns; of one to four times as
+    // many units as workgroups, what leaves the least idle.
     const int64_t all = int64_t(a.groups) * a.samples;
-    a.pg = int(std::max<int64_t>(1, std::min<int64_t>(4 / a.nw, (all + 511) / 512)));
-    const int64_t grid = (all + a.pg - 1) / a.pg;
-    a.grid = int(std::min<int64_t>(grid, 256 * std::clamp(8 / (a.nw * a.pg), 1, 2)));
-    // Units: slices of a sample's groups.  Walkers take them in turns; of one to four times as
-    // many units as walkers, what leaves the least idle.
-    const int walkers = a.grid * a.pg;
-    a.slices = std::min(walkers, a.groups);
+    a.pg = int(std::max<int64_t>(1, std::min<int64_t>(std::max(1, 4 / a.nw), (all + 511) / 512)));
+    a.grid = int(std::min<int64_t>((all + a.pg - 1) / a.pg, 256 * std::clamp(8 / (a.nw * a.pg), 1, 4)));
+    const int most = (a.groups + a.pg - 1) / a.pg;
+    a.slices = std::min(a.grid, most);
     if (a.gate) {
         int64_t best = 0;
         for (int k = 1; k <= 4; ++k) {
-            const int64_t s = std::max<int64_t>(1, std::min<int64_t>(a.groups, int64_t(k) * walkers / a.samples));
-            const int64_t turns = (s * a.samples + walkers - 1) / walkers * ((a.groups + s - 1) / s);
+            const int64_t s = std::max<int64_t>(1, std::min<int64_t>(most, int64_t(k) * a.grid / a.samples));
+            const int64_t turns = (s * a.samples + a.grid - 1) / a.grid * ((most + s - 1) / s);
             if (!best || turns < best) {
                 best = turns;
                 a.slices = int(s);
@@ -185,7 +312,22 @@ void join_plan(JoinArgs& a, bool backward) {
 
 hipError_t launch_join_fwd(const JoinArgs& a, hipStream_t s) {
     const unsigned x = unsigned(std::min(a.grid, 1 << 22));     // threads of a dimension: 32 bits
-    DC_JOIN_LAUNCH(join_fwd_kernel, 2, a, dim3(x, (unsigned(a.grid) + x - 1) / x), s);
+    const dim3 g(x, (unsigned(a.grid) + x - 1) / x), b(64 * a.nw * a.pg);
+    if (a.cl) {
+        if (a.lpx == 16) hipLaunchKernelGGL((join_rows_fwd_kernel<16, 1>), g, b, 0, s, a);
+        else if (a.lpx == 8) hipLaunchKernelGGL((join_rows_fwd_kernel<8, 1>), g, b, 0, s, a);
+        else if (a.lpx == 4) hipLaunchKernelGGL((join_rows_fwd_kernel<4, 1>), g, b, 0, s, a);
+        else if (a.lpx == 2) hipLaunchKernelGGL((join_rows_fwd_kernel<2, 1>), g, b, 0, s, a);
+        else if (a.held == 1) hipLaunchKernelGGL((join_rows_fwd_kernel<1, 1>), g, b, 0, s, a);
+        else if (a.held == 2) hipLaunchKernelGGL((join_rows_fwd_kernel<1, 2>), g, b, 0, s, a);
+        else hipLaunchKernelGGL((join_rows_fwd_kernel<1, 0>), g, b, 0, s, a);
+    } else if (a.lpx == 64) {
+        if (a.held == 1) hipLaunchKernelGGL((join_fwd_kernel<64, 1>), g, b, 0, s, a);
+        else hipLaunchKernelGGL((join_fwd_kernel<64, 2>), g, b, 0, s, a);
+    } else {
+        if (a.held == 1) hipLaunchKernelGGL((join_fwd_kernel<16, 1>), g, b, 0, s, a);
+        else hipLaunchKernelGGL((join_fwd_kernel<16, 0>), g, b, 0, s, a);
+    }
     return hipGetLastError();
 }
 
