@@ -212,32 +212,23 @@ __global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
     if constexpr (R) each_eight<R>(a, l, join);
     float mu2 = 0, r2 = 0;
     if (a.pre.kind) moments(a.pre, 2, mu2, r2, join);
-    // the four lanes of a block of 32 channels stay together: its scale is theirs
+    if (a.q) {       // the four lanes of a block of 32 channels together, also those past the last eight
+        for (int i = 0, e = l.unit; e < a.blocks * 4; e += l.ng, ++i) {
+            float o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (8 * e < a.C) {
+                if constexpr (!R) join(0, e);
+#pragma unroll
+                for (int k = 0; k < H; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) o[j] = k == i || !R ? v[k][j] : o[j];
+            }
+            q8_store_eight(a.q, a.qm, p, e, in, a.C, o);
+        }
+    }
     each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) {
         const int c0 = 8 * e;
         if constexpr (!R) join(0, e);
         if (in) store8<true>(a.o, p, c0, a.C, v[i]);
-        if (a.q) {
-            uint32_t top = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = max(top, abs_bits(v[i][j]));
-            // lanes past the last eight hold nothing and are not here: they read as 0 or as themselves
-#pragma unroll
-            for (int d = 1; d < 4; d *= 2) {
-                const uint32_t other = __shfl_xor(top, d);
-                top = max(top, (e ^ d) * 8 < a.C ? other : 0u);
-            }
-            const uint32_t s = q8_scale(top);
-            const float per = q8_per(s);
-            const int64_t at = int64_t(c0 / 32) * a.qm.HW + p.pix;
-            if (in) {
-                uint2* d = reinterpret_cast<uint2*>(a.q + p.n * a.qm.qn + at * 32 + c0 % 32);
-                *d = make_uint2(q8_pack(v[i][0], v[i][1], v[i][2], v[i][3], per), q8_pack(v[i][4], v[i][5], v[i][6], v[i][7], per));
-                if (e % 4 == 0) reinterpret_cast<uint8_t*>(a.q)[a.qm.s0 + p.n * a.qm.sn + at] = uint8_t(s);
-                if (c0 + 8 >= a.C)      // the block's channels past the last lane's
-                    for (int k = e % 4 + 1; k < 4; ++k) d[k - e % 4] = make_uint2(0, 0);
-            }
-        }
         if (a.pre.kind && a.u.p) {
             float g[8], b[8];
             params8<false>(g, a.pre.gamma, c0, a.C, 1.0f);

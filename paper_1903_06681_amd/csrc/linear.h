@@ -98,19 +98,20 @@ enum { WEIGHT, PIXEL, LONG, PAIR };   // which way an operand is found: see Stag
 
 static constexpr int kRow = 128;   // bytes of k a slice
 
-// The shape of a workgroup's block: BM x BN of the result, NST slices in LDS (2, or 1 where
-// there is only one), WM x WN waves; OCC waves a SIMD that the registers leave room for.
-template <typename T_, int BM_, int BN_, int NST_, int WM_, int WN_, int OCC_>
+// The shape of a workgroup's block: BM x BN of the result, NST slices in LDS (2 or 3, or 1 where
+// there is only one) of KB bytes of k, WM x WN waves; OCC waves a SIMD that the registers leave
+// room for.
+template <typename T_, int BM_, int BN_, int NST_, int WM_, int WN_, int OCC_, int KB_ = kRow>
 struct Shape {
     typedef T_ T;
-    static constexpr int BM = BM_, BN = BN_, NST = NST_, WM = WM_, WN = WN_, OCC = OCC_;
-    static constexpr int E = 16 / int(sizeof(T)), BK = kRow / int(sizeof(T));
-    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32, GROUPS = kRow / 32;
-    static constexpr int ABYTES = BM * kRow, BYTES = (BM + BN) * kRow;
+    static constexpr int BM = BM_, BN = BN_, NST = NST_, WM = WM_, WN = WN_, OCC = OCC_, KB = KB_;
+    static constexpr int E = 16 / int(sizeof(T)), BK = KB / int(sizeof(T));
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32, GROUPS = KB / 32;
+    static constexpr int ABYTES = BM * KB, BYTES = (BM + BN) * KB;
     static constexpr int TH = 64 * WM * WN;
 };
 
-// ---- staging of one operand's slice: R rows by 128 bytes of k.
+// ---- staging of one operand's slice: R rows by KB bytes of k.
 //   WEIGHT  a matrix, rows [row][k] (RK) or [k][row] (KR)
 //   PIXEL   rows are slots: k the channels' planes (KR), or contiguous (RK: rows of channels)
 //   LONG    k runs over the slots, rows are channels: planes (RK), or rows of channels (KR)
@@ -119,11 +120,11 @@ struct Shape {
 // A thread's chunks of 16 bytes follow each other in LDS at a distance of the
 // workgroup; which chunk of memory they hold is permuted, so that LDS is written in
 // order (as direct loads must) and read without bank conflicts.
-template <typename T, int KIND, int SRC, int R, int TH>
+template <typename T, int KIND, int SRC, int R, int TH, int KB = kRow>
 struct Stage {
     static constexpr int E = 16 / int(sizeof(T));
-    static constexpr int CPR = KIND == RK ? kRow / 16 : R / E;  // chunks of an LDS row
-    static constexpr int U = R * kRow / 16 / TH;       // chunks a thread
+    static constexpr int CPR = KIND == RK ? KB / 16 : R / E;    // chunks of an LDS row
+    static constexpr int U = R * KB / 16 / TH;         // chunks a thread
     static constexpr int STEP = TH / CPR;              // LDS rows between them
     // pointers a thread keeps: one for all chunks where they lie at equal distances
     static constexpr int P = SRC == PIXEL && KIND == RK ? U : 1;
@@ -134,7 +135,7 @@ struct Stage {
 
     // the permutation of an LDS row's chunks; the same for all rows of a thread
     __device__ __forceinline__ static int mix(int row) {
-        if constexpr (KIND == RK) return (row >> 1) & 7;   // 16 lanes, 256 bytes a cycle
+        if constexpr (KIND == RK) return KB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;   // 16 lanes, 256 bytes a cycle
         else if constexpr (sizeof(T) == 2) return R >= 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
         else return 0;
     }
@@ -148,9 +149,10 @@ struct Stage {
         left = E;
         bool in = true;
         if constexpr (SRC == PAIR) {               // first: of the pair
-            static_assert(KIND == RK && (STEP <= 32 || STEP == 64));
-            at[0] = int64_t(first + r0 % 32 + (r0 / 32 ? o.rows : 0)) * o.ld + c * E;
-            left = o.rows - (first + r0 % 32);
+            static_assert(KIND == RK && (STEP <= 32 || STEP % 64 == 0));
+            const int row = first + r0 / 64 * 32 + r0 % 32;
+            at[0] = (int64_t(row) + (r0 / 32 % 2 ? o.rows : 0)) * o.ld + c * E;
+            left = o.rows - row;
         } else if constexpr (SRC == WEIGHT && KIND == RK) {
             at[0] = int64_t(first + r0) * o.ld + c * E;
             left = o.rows - (first + r0);          // rows from this one on
@@ -179,9 +181,9 @@ struct Stage {
     }
 
     // PAIR: row of chunk i after chunk 0's; whether it is one of the second matrix (of the other, where
-    // a thread's chunks lie 64 rows apart)
+    // a thread's chunks lie whole pairs of groups apart)
     __device__ __forceinline__ static constexpr int pair_row(int i) {
-        return STEP == 64 ? i * 32 : (i * STEP / 32) / 2 * 32 + i * STEP % 32;
+        return STEP >= 64 ? i * STEP / 2 : (i * STEP / 32) / 2 * 32 + i * STEP % 32;
     }
     __device__ __forceinline__ static constexpr bool pair_second(int i) { return STEP < 64 && (i * STEP / 32) % 2; }
 
@@ -250,9 +252,9 @@ struct Stage {
 // ---- fragments.  k-group g: 16 (bf16) or 8 (fp32) values of k.  bf16: lane l
 // holds row l % 32, k 8 (l / 32) .. + 7.  fp32: k 4 (l / 32) + i for i = 0 .. 3,
 // one matrix instruction each.
-template <typename T, int KIND, int R, int TH>
+template <typename T, int KIND, int R, int TH, int KB = kRow>
 __device__ __forceinline__ void fragment(uint4& f, const char* lds, int row0, int g, int lane) {
-    typedef Stage<T, KIND, WEIGHT, R, TH> S;
+    typedef Stage<T, KIND, WEIGHT, R, TH, KB> S;
     const int h = lane >> 5, r = lane & 31;
     if constexpr (KIND == RK) {
         f = *reinterpret_cast<const uint4*>(lds + S::lds_at(row0 + r, 2 * g + h));
@@ -292,19 +294,19 @@ __device__ __forceinline__ void multiply(f32x16_t& acc, const uint4& a, const ui
 // A wave reads the next k-group's fragments while it multiplies the last read one's, also
 // from one slice to the next: before a slice's last group every wave has read all of it
 // (one barrier a slice), so its buffer is free and the next one's is in place.  DIRECT:
-// slices come straight into LDS; else through registers.
+// slices come straight into LDS; else through registers.  rot: the slice that comes first.
 template <typename S, int AK, int BK_, bool DIRECT, typename SA, typename SB, typename F>
 __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const SA& sa, const SB& sb, const Operand& oa,
                                           const Operand& ob, const Slots& s, int k0, int k1, char (*lds)[S::BYTES], int row0,
-                                          int col0, int lane, F&& seen) {
+                                          int col0, int lane, F&& seen, int rot = 0) {
     typedef typename S::T T;
     constexpr int NST = S::NST;
     uint4 fa[2][S::TM], fb[2][S::TN];
     auto read = [&](int to, const char* a, int g) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < S::TM; ++i) fragment<T, AK, S::BM, S::TH>(fa[to][i], a, row0 + 32 * i, g, lane);
+        for (int i = 0; i < S::TM; ++i) fragment<T, AK, S::BM, S::TH, S::KB>(fa[to][i], a, row0 + 32 * i, g, lane);
 #pragma unroll
-        for (int j = 0; j < S::TN; ++j) fragment<T, BK_, S::BN, S::TH>(fb[to][j], a + S::ABYTES, col0 + 32 * j, g, lane);
+        for (int j = 0; j < S::TN; ++j) fragment<T, BK_, S::BN, S::TH, S::KB>(fb[to][j], a + S::ABYTES, col0 + 32 * j, g, lane);
     };
     auto multiply_group = [&](int from) __attribute__((always_inline)) {
 #pragma unroll
@@ -317,10 +319,16 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
     const uint32_t base = lds_address(lds[0]);
     const bool whole = sa.whole && sb.whole;
     const int n = (k1 - k0 + S::BK - 1) / S::BK;       // steps
+    // slice by slice from the rot-th on, then the first ones
+    auto slice_k = [&](int step) __attribute__((always_inline)) {
+        const int t = step + rot;
+        return k0 + (t >= n ? t - n : t) * S::BK;
+    };
+    auto all_there = [&](int step) __attribute__((always_inline)) { return whole && slice_k(step) + S::BK <= k1; };
     auto fetch = [&](int step, int buf) __attribute__((always_inline)) {
         const uint32_t to = base + buf * S::BYTES;
-        const int k = k0 + step * S::BK;
-        if (whole && k + S::BK <= k1) {
+        const int k = slice_k(step);
+        if (all_there(step)) {
             sa.template fetch<true>(oa, s, k, lds[buf], to);
             sb.template fetch<true>(ob, s, k, lds[buf] + S::ABYTES, to + S::ABYTES);
         } else {
@@ -330,7 +338,7 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
     };
     uint4 va[SA::U], vb[SB::U];
     auto load = [&](int step) __attribute__((always_inline)) {
-        const int k = k0 + step * S::BK;
+        const int k = slice_k(step);
         sa.load(va, oa, s, k);
         sb.load(vb, ob, s, k);
     };
@@ -338,20 +346,35 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
         sa.store(va, lds[buf]);
         sb.store(vb, lds[buf] + S::ABYTES);
     };
+    // Slice `step` is there: of the direct loads only those of the slice after it may be on
+    // their way (as many as chunks, where all of its are there; three slices).
+    auto wait_for = [&](int step) __attribute__((always_inline)) {
+        if constexpr (NST == 3) {
+            if (step + 1 < n && all_there(step + 1)) {
+                asm volatile("s_waitcnt vmcnt(%0)" :: "n"(SA::U + SB::U) : "memory");
+                return;
+            }
+        }
+        wait_direct();
+    };
     if constexpr (DIRECT) {
         fetch(0, 0);
-        wait_direct();
+        if (NST == 3 && 1 < n) fetch(1, 1);
+        wait_for(0);
     } else {
         load(0);
         store(0);
         if (1 < n) load(1);
     }
     __syncthreads();
-    if (DIRECT && NST > 1 && 1 < n) fetch(1, 1);
+    if (DIRECT && NST > 1 && NST - 1 < n) fetch(NST - 1, NST - 1);
     read(0, lds[0], 0);
-    for (int step = 0, buf = 0; step < n; ++step, buf ^= 1) {
-        const int next = buf ^ 1;
+    for (int step = 0, buf = 0; step < n; ++step) {
+        const int next = NST == 1 ? 0 : buf + 1 == NST ? 0 : buf + 1;
         const bool more = step + 1 < n;
+        // The slice's first fragments were read before the last products and are there: said so here,
+        // else the compiler, which does not follow them round the loop, waits for the next ones too
+        __builtin_amdgcn_s_waitcnt(0xc07f);     // lgkmcnt(0)
         if (!DIRECT && NST > 1 && more) {
             store(next);
             if (step + 2 < n) load(step + 2);
@@ -361,15 +384,16 @@ __device__ __forceinline__ void tile_loop(f32x16_t (&acc)[S::TM][S::TN], const S
             if constexpr (g + 1 < S::GROUPS) {
                 read((g + 1) & 1, lds[buf], g + 1);
             } else if (NST > 1 && more) {
-                if (DIRECT) wait_direct();
+                if (DIRECT) wait_for(step + 1);
                 __syncthreads();
-                if (DIRECT && step + 2 < n) fetch(step + 2, buf);
+                if (DIRECT && step + NST < n) fetch(step + NST, buf);
                 read(0, lds[next], 0);
             }
             __builtin_amdgcn_sched_barrier(0);
             multiply_group(g & 1);
             __builtin_amdgcn_sched_barrier(0);
         });
+        buf = next;
     }
 }
 
