@@ -74,8 +74,8 @@ dc_status dc_dropout(const dc_drop* drop, const dc_view* vx, const void* x, cons
     a.rows = t.rows();
     a.HW = vx->H * vx->W;
     a.len = a.rows ? 1 : t.flat() ? a.HW : vx->W;
-    const int V = dropout_chunk(a.x, a.y, a.rows);
-    a.cpr = (a.len - 1) / V + 1;
+    a.per = dropout_chunk(a.x, a.y, a.rows, pixels_of(*vx), a.d.groups);
+    a.cpr = (a.len - 1) / a.per + 1;
     a.chunks = vx->N * (a.HW / a.len) * a.cpr;
     a.dsample = fast_div(uint32_t(a.HW / a.len * a.cpr));
     a.dcpr = fast_div(uint32_t(a.cpr));

@@ -62,11 +62,12 @@ struct DropoutArgs {
     View x, y;
     DropArgs d;
     int32_t C, HW, len;        // pixels of a sample, of a row of the numbering
-    int32_t chunks, cpr;       // chunks of pixels in all, of a row
+    int32_t per;               // pixels of a chunk
+    int32_t chunks, cpr;       // chunks in all, of a row
     FastDiv dsample, dcpr;     // chunks of a sample, of a row
     int32_t rows;              // rows of channels
 };
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t s);
-int dropout_chunk(const View& x, const View& y, bool rows);    // pixels a thread takes
+int dropout_chunk(const View& x, const View& y, bool rows, int64_t pixels, int groups);    // pixels a thread takes
 
 }  // namespace dc

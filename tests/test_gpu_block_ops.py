@@ -63,6 +63,17 @@ def test_dropout(shape, layout, types, place):
     assert A.untouched(y, mem)
 
 
+# 16 bytes a thread: 2048 waves and more; eights of channels in two workgroups' widths
+DROP_SIZES = [((2, 64, 150, 151), "dense"), ((1, 100, 213, 211), "gaps"), ((3, 43, 200, 230), "padded"), ((40, 2500, 30, 1), "rows"),
+              ((3, 520, 333, 1), "slice")]
+
+
+@pytest.mark.parametrize("shape,layout", DROP_SIZES, ids=str)
+@pytest.mark.parametrize("types", ["f32-f32", "bf16-bf16", "f32-bf16", "bf16-f32"])
+def test_dropout_sizes(shape, layout, types):
+    test_dropout(shape, layout, types, {"h0": 1, "w0": 2, "H": 1000, "W": 999})
+
+
 def test_dropout_in_place_of_everything_and_nothing():
     g = rng(2)
     x = randn(g, 2, 20, 6, 9).cuda()
