@@ -58,6 +58,11 @@ __device__ __forceinline__ bool kept(const Philox& p, int j, int t) {
     return j & 1 ? p.w[j / 2] >= uint32_t(t) << 16 : uint16_t(p.w[j / 2]) >= uint16_t(t);
 }
 
+// v where bit j is set, else 0, whatever v is
+__device__ __forceinline__ float masked(float v, uint32_t bits, int j) {
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & uint32_t(int32_t(bits << (31 - j)) >> 31));
+}
+
 struct DropoutArgs {
     View x, y;
     DropArgs d;

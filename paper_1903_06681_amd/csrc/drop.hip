@@ -61,9 +61,6 @@ __device__ __forceinline__ uint32_t mask8(const DropArgs& d, const DropPixel& p,
     for (int j = 0; j < 8; ++j) b |= kept(w, j, d.t) ? 1u << j : 0u;
     return b;
 }
-__device__ __forceinline__ float masked(float v, uint32_t bits, int j) {
-    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & uint32_t(int32_t(bits << (31 - j)) >> 31));
-}
 
 // planes: V pixels of a row, eight channels
 template <typename XT, typename YT, int V>

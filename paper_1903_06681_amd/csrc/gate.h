@@ -19,6 +19,7 @@ struct GateArgs {
     LinearArgs l;      // z: zg; out: h (forward) or dz (backward, of 2 K channels); rows: K
     View zu;           // beside l.z, of its layout
     int32_t rows_kept; // rows of blocks that an XCD goes through the columns with
+    FastDiv dset, drows, drest;   // blocks of such a set; its rows; the last set's rows
     DropArgs drop;
 };
 hipError_t launch_gate_fwd(const GateArgs& a, bool f32, hipStream_t s);
@@ -26,23 +27,24 @@ hipError_t launch_gate_bwd(const GateArgs& a, bool f32, hipStream_t s);
 bool gate_few(const GateArgs& a, bool bwd, bool f32);
 hipError_t launch_gate_few(const GateArgs& a, bool bwd, bool f32, hipStream_t s);
 
-// Dropout of the lane's 16 channels of a block (first: o0): 8 g + 4 h .. + 3 for g = 0 .. 3.
-// A call of the generator serves eight channels, half of them the partner lane's (32 on):
-// each half wave makes two of the four calls, and they trade halves.
-__device__ __forceinline__ void drop_half(float (&v)[16], const DropArgs& d, const DropPixel& p, int o0, int h) {
+// The mask of the lane's 16 channels of a block (first: o0), 8 g + 4 h .. + 3 for g = 0 .. 3, a bit each.  A call of the generator serves eight channels, half of them the partner lane's (32
+// on): each half wave makes two of the four calls, and they trade halves.
+__device__ __forceinline__ uint32_t bits_half(const DropArgs& d, const DropPixel& p, int o0, int h) {
+    uint32_t bits = 0;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int g = k + 2 * h;
-        Philox w = philox(p.pos + uint64_t(o0 / 8 + g) * uint64_t(d.plane), p.ctr, d.seed);
-        // w[0], w[1]: words 2 h and 2 h + 1 of call k; w[2], w[3]: of call k + 2
+    for (int i = 0; i < 2; ++i) {
+        Philox w = philox(p.pos + uint64_t(o0 / 8 + i + 2 * h) * uint64_t(d.plane), p.ctr, d.seed);
+        // w[0], w[1]: words 2 h and 2 h + 1 of call i; w[2], w[3]: of call i + 2
         swap_halves(w.w[0], w.w[2]);
         swap_halves(w.w[1], w.w[3]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = 4 * (k + 2 * (j / 4)) + j % 4;
-            v[r] = kept(w, j, d.t) ? v[r] * d.scale : 0.0f;
-        }
+        for (int j = 0; j < 8; ++j) bits |= kept(w, j, d.t) ? 1u << (4 * (i + 2 * (j / 4)) + j % 4) : 0u;
     }
+    return bits;
+}
+__device__ __forceinline__ void drop_half(float (&v)[16], uint32_t bits, float scale) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = masked(v[r] * scale, bits, r);
 }
 
 __device__ __forceinline__ void clear_past(float (&v)[16], int o0, int h, int rows) {
@@ -63,7 +65,20 @@ __device__ __forceinline__ void gate_epilogue(float (&f)[16], float (&u)[16], co
                                               const DropPixel& dp, int o0, int lane) {
     const LinearArgs& l = a.l;
     const int pix = p.c.r * l.s.len + p.w, h = lane >> 5;
-    if (l.bias) {
+    if (l.bias && o0 + 32 <= l.rows) {
+        typedef float f32x4_at __attribute__((ext_vector_type(4), aligned(4)));
+        const float* from = l.bias + o0 + 4 * h;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4_at bf = *reinterpret_cast<const f32x4_at*>(from + 8 * g);
+            const f32x4_at bu = *reinterpret_cast<const f32x4_at*>(from + l.rows + 8 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                f[4 * g + r] += bf[r];
+                u[4 * g + r] += bu[r];
+            }
+        }
+    } else if (l.bias) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int c = min(o0 + 8 * (r / 4) + 4 * h + r % 4, l.rows - 1);
@@ -85,7 +100,7 @@ __device__ __forceinline__ void gate_epilogue(float (&f)[16], float (&u)[16], co
     apply_act(f, l.act);
 #pragma unroll
     for (int r = 0; r < 16; ++r) f[r] *= u[r];
-    if (a.drop.t) drop_half(f, a.drop, dp, o0, h);
+    if (a.drop.t) drop_half(f, bits_half(a.drop, dp, o0, h), a.drop.scale);
     store_half(f, l.out, p, o0, lane, l.rows);
 }
 
@@ -101,23 +116,24 @@ __device__ __forceinline__ void gate_slope(float (&v)[16], const GateArgs& a, co
         load_half(f, l.z, p, o0, lane, l.rows);
         load_half(u, a.zu, p, o0, lane, l.rows);
     }
-    if (a.drop.t) drop_half(v, a.drop, dp, o0, h);
     float g[16];           // dzg
+    const uint32_t bits = a.drop.t ? bits_half(a.drop, dp, o0, h) : 0;
+    if (a.drop.t) drop_half(v, bits, a.drop.scale);
 #pragma unroll
     for (int r = 0; r < 16; ++r) g[r] = v[r] * u[r];
     apply_slope(f, g, l.act);
+    if (l.h.dt >= 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) u[r] *= f[r];
+        if (a.drop.t) drop_half(u, bits, a.drop.scale);
+        store_half(u, l.h, p, o0, lane, l.rows);
+    }
     View out = l.out;
     store_half(g, out, p, o0, lane, l.rows);
 #pragma unroll
     for (int r = 0; r < 16; ++r) v[r] *= f[r];
     out.p += l.rows * out.sc * (out.dt == DC_F32 ? 4 : 2);
     store_half(v, out, p, o0, lane, l.rows);
-    if (l.h.dt >= 0) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) f[r] *= u[r];
-        if (a.drop.t) drop_half(f, a.drop, dp, o0, h);
-        store_half(f, l.h, p, o0, lane, l.rows);
-    }
 }
 
 // The same for eight channels of one pixel a lane (rows of channels; four neighbouring lanes hold a
@@ -279,8 +295,10 @@ __global__ __launch_bounds__(S::TH, S::OCC) void gate_kernel(GateArgs a) {
     // Blocks of as many rows as half an XCD's L2 holds the weights of, column by column, then the
     // next rows: an XCD keeps to its rows' weights while the pixels stream by.
     const int id = xcd_range(blockIdx.x, l.tr * l.tc);
-    const int set = id / (a.rows_kept * l.tc), in_set = id - set * a.rows_kept * l.tc, rows = min(a.rows_kept, l.tr - set * a.rows_kept);
-    const int tc = in_set / rows, tr = set * a.rows_kept + in_set - tc * rows;
+    const int set = int(a.dset.div(uint32_t(id))), in_set = id - set * int(a.dset.d);
+    const bool rest = (set + 1) * a.rows_kept > l.tr;
+    const int tc = int(rest ? a.drest.div(uint32_t(in_set)) : a.drows.div(uint32_t(in_set)));
+    const int tr = set * a.rows_kept + in_set - tc * int(rest ? a.drest.d : a.drows.d);
     const int first = tr * (S::BM / PAIRS);          // of the block's channels
     Stage<T, AK, BWD ? WEIGHT : PAIR, S::BM, S::TH, S::KB> sa;
     Stage<T, PK, PIXEL, S::BN, S::TH, S::KB> sb;
@@ -494,6 +512,9 @@ static void launch_gate_shape(GateArgs a, hipStream_t s) {
     a.l.tr = ((rows + (BWD ? 0 : 63)) / (BWD ? 1 : 64) * (BWD ? 1 : 64) + S::BM - 1) / S::BM;
     a.l.tc = int((int64_t(a.l.s.chunks) * a.l.s.per + S::BN - 1) / S::BN);
     a.rows_kept = int(std::clamp<int64_t>((2 << 20) / (int64_t(S::BM) * a.l.a.red * int64_t(sizeof(typename S::T))), 1, a.l.tr));
+    a.dset = fast_div(uint32_t(a.rows_kept) * uint32_t(a.l.tc));
+    a.drows = fast_div(uint32_t(a.rows_kept));
+    a.drest = fast_div(uint32_t(a.l.tr % a.rows_kept ? a.l.tr % a.rows_kept : a.rows_kept));
     const dim3 g(unsigned(a.l.tr) * unsigned(a.l.tc)), t(S::TH);
     if (a.l.cl && a.l.direct) hipLaunchKernelGGL((gate_kernel<S, BWD, true, true>), g, t, 0, s, a);
     else if (a.l.cl) hipLaunchKernelGGL((gate_kernel<S, BWD, true, false>), g, t, 0, s, a);
