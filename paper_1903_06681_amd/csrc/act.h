@@ -17,7 +17,7 @@ namespace dc {
 // m = 0 stands for d = 1.
 struct FastDiv {
     uint32_t m, sh, d;
-    __device__ __forceinline__ uint32_t div(uint32_t n) const { return m ? __umulhi(n, m) >> sh : n; }
+    __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) >> sh) + (m ? 0 : n); }   // no branch
 };
 
 inline FastDiv fast_div(uint32_t d) {

@@ -26,15 +26,16 @@ struct DropPixel {
     uint64_t pos, ctr;         // counter of the first eight channels, its upper half
 };
 
-__device__ __forceinline__ DropPixel drop_pixel(const DropArgs& d, int n, int pix) {
+__device__ __forceinline__ uint64_t drop_counter(const DropArgs& d) { return d.offset + (d.step ? *d.step : 0); }
+__device__ __forceinline__ uint64_t drop_position(const DropArgs& d, int n, int pix) {
     const int tile = int(d.per.div(uint32_t(n))), tp = int(d.dQ.div(uint32_t(tile)));
     const int r = int(d.dW.div(uint32_t(pix)));
     const int64_t s = d.n0 + int64_t(n - tile * int(d.per.d));
     const int64_t h = d.h0 + int64_t(tp) * d.H + r, w = d.w0 + int64_t(tile - tp * d.Q) * d.W + (pix - r * d.W);
-    DropPixel p;
-    p.pos = uint64_t(s * d.groups * d.plane + h * d.cols + w);
-    p.ctr = d.offset + (d.step ? *d.step : 0);
-    return p;
+    return uint64_t(s * d.groups * d.plane + h * d.cols + w);
+}
+__device__ __forceinline__ DropPixel drop_pixel(const DropArgs& d, int n, int pix) {
+    return DropPixel{drop_position(d, n, pix), drop_counter(d)};
 }
 
 // four words for eight channels

@@ -32,7 +32,8 @@ struct JoinArgs {
     float* stat;                   // [4][pixels]: mean and 1 / deviation of y, of o; null (forward): not kept
     float invC;
     int32_t C, blocks;
-    int32_t lpx, nw, pg, held;     // as in NormArgs; held: blocks of 32 or eights of channels
+    int32_t eights;                // lanes of eight channels, else of 32
+    int32_t lpx, nw, pg, held;     // as in NormArgs; held: eights, or blocks of 32 channels
     int32_t grid, cl;
     int32_t groups;                // pixel groups (backward: of a sample, or of all pixels where there is no gate)
     // backward: parameters' gradients
@@ -48,66 +49,28 @@ size_t join_bwd_part_bytes(int N, int HW, int C, bool gate);
 hipError_t launch_join_fwd(const JoinArgs& a, hipStream_t s);
 hipError_t launch_join_bwd(const JoinArgs& a, hipStream_t s);
 
-// a block of 32 as it lies in memory; channels past C repeat the last one
-template <bool CL>
-__device__ __forceinline__ void load_raw(uint32_t (&w)[32], const View& t, const Q8Map& qm, const Pixel& p, int c0, int C) {
-    if (t.dt == DC_Q8) {
-        const int64_t at = int64_t(c0 / 32) * qm.HW + p.pix;
-        const uint4* d = reinterpret_cast<const uint4*>(t.p + p.n * qm.qn + at * 32);
-        const uint4 a = d[0], b = d[1];
-        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-        w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-        w[8] = reinterpret_cast<const uint8_t*>(t.p)[qm.s0 + p.n * qm.sn + at];
-        return;
-    }
+// Planes: a block of 32 channels as it lies in memory; channels past C repeat the last one
+__device__ __forceinline__ void load_raw(uint32_t (&w)[32], const View& t, const Pixel& p, int c0, int C) {
     const int es = t.dt == DC_F32 ? 4 : 2;
-    char* a = t.p + (p.n * t.sn + p.h * t.sh + p.w + c0 * (CL ? 1 : t.sc)) * es;
-    if constexpr (CL) {
-        if (c0 + 32 <= C) {
-            const int n = es == 4 ? 8 : 4;
+    char* a = t.p + (p.n * t.sn + p.h * t.sh + p.w + c0 * t.sc) * es;
+    const int64_t step = t.sc * es;
+    if (es == 4) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < n) {
-                    const u32x4_any u = *reinterpret_cast<const u32x4_any*>(a + 16 * j);
-                    w[4 * j] = u.x, w[4 * j + 1] = u.y, w[4 * j + 2] = u.z, w[4 * j + 3] = u.w;
-                }
-        } else if (es == 4) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) w[j] = reinterpret_cast<const uint32_t*>(a)[min(j, C - 1 - c0)];
-        } else {
-            const uint16_t* e = reinterpret_cast<const uint16_t*>(a);
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                w[j] = e[min(2 * j, C - 1 - c0)] | uint32_t(e[min(2 * j + 1, C - 1 - c0)]) << 16;
-        }
+        for (int j = 0; j < 32; ++j, next(a, c0 + j < C ? step : 0)) w[j] = *reinterpret_cast<const uint32_t*>(a);
     } else {
-        const int64_t step = t.sc * es;
-        if (es == 4) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j, next(a, c0 + j < C ? step : 0)) w[j] = *reinterpret_cast<const uint32_t*>(a);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j, next(a, c0 + j < C ? step : 0)) w[j] = *reinterpret_cast<const uint16_t*>(a);
-        }
+        for (int j = 0; j < 32; ++j, next(a, c0 + j < C ? step : 0)) w[j] = *reinterpret_cast<const uint16_t*>(a);
     }
 }
 
 // its values; channels past C are zero
-template <bool CL>
 __device__ __forceinline__ void raw_values(float (&v)[32], const uint32_t (&w)[32], const View& t, int c0, int C) {
-    if (t.dt == DC_Q8) {
-        const float step = q8_step(w[8]);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = q8_value(w[j / 4], j % 4, step);
-    } else if (t.dt == DC_F32) {
+    if (t.dt == DC_F32) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = __builtin_bit_cast(float, w[j]);
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            if constexpr (CL) v[j] = __builtin_bit_cast(float, j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
-            else v[j] = __builtin_bit_cast(float, w[j] << 16);
-        }
+        for (int j = 0; j < 32; ++j) v[j] = __builtin_bit_cast(float, w[j] << 16);
     }
     if (c0 + 32 > C) {
 #pragma unroll

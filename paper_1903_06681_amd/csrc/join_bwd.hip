@@ -37,6 +37,7 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
     const bool has_pre = a.pre.kind && a.du.p, has_post = a.post.kind != DC_NORM_NONE;
     const bool want_pre = has_pre && (a.dgpre || a.dbpre), want_post = has_post && (a.dgpost || a.dbpost);
     const bool want_scale = a.dscale || a.dgate;
+    const uint64_t counter = a.drop.t ? drop_counter(a.drop) : 0;     // read once: in the loop its wait would be the tensors' too
     const int width = a.blocks * 32, wg = CL ? int(blockIdx.x) : xcd_range(blockIdx.x, a.grid);
     // Sums of a lane's eight channels over the workgroup's pixels, from all its lanes and waves,
     // to the eight floats of `to`; every wave comes here.  R = 0: added to what is there.
@@ -195,18 +196,28 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
                 k = fetch_moments(m);
                 if constexpr (R > 1) each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) { fetch(w, i, p, e); });
             }
+            // lanes without a pixel hold another one's, with gradients of zero: nothing for the sums
+            if constexpr (R != 0) {
+                if (!__all(in)) {
+#pragma unroll
+                    for (int i = 0; i < H; ++i) w.d[i] = in ? w.d[i] : u32x8{0, 0, 0, 0, 0, 0, 0, 0}, w.r[i] = in ? w.r[i] : u32x8{0, 0, 0, 0, 0, 0, 0, 0};
+                }
+            }
             const float mu1 = k.mu1, r1 = k.r1, mu2 = k.mu2, r2 = k.r2;
             DropPixel dp{};
             {
                 const JoinArgs& b = fresh();
-                if (b.drop.t) dp = drop_pixel(b.drop, p.n, p.pix);
+                if (b.drop.t) dp = DropPixel{drop_position(b.drop, p.n, p.pix), counter};
             }
             // o's normed value; du, then dO, then dv; y's normed value (y without a norm); drop of what the
             // factor multiplies; the mask's factors
             float vo[H][8], vd[H][8], vy[H][8], vt[H][8], keep[H][8];
             auto open = [&](int i, int e) __attribute__((always_inline)) {
                 const int c0 = 8 * e;
-                if constexpr (!R) fetch(w, 0, p, e);
+                if constexpr (!R) {
+                    fetch(w, 0, p, e);
+                    w.d[0] = in ? w.d[0] : u32x8{0, 0, 0, 0, 0, 0, 0, 0}, w.r[0] = in ? w.r[0] : u32x8{0, 0, 0, 0, 0, 0, 0, 0};
+                }
                 {
                     const JoinArgs& b = fresh();
                     keep8(keep[i], b.drop, dp, e);
@@ -219,7 +230,7 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
                 for (int j = 0; j < 8; ++j) vy[i][j] = (vy[i][j] - mu1) * r1;
                 if (has_post) clear8(vy[i], c0, fresh().C);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) vt[i][j] = dropped(has_post ? fmaf(g[j], vy[i][j], t[j]) : vy[i][j], keep[i][j]);
+                for (int j = 0; j < 8; ++j) vt[i][j] = dropped(fmaf(g[j], vy[i][j], t[j]), keep[i][j]);    // 1 and 0 without a norm
                 if (!has_pre) return;
                 const JoinArgs& b = fresh();
                 values8<CL>(vo[i], w.o[i], b.x, c0, b.C);
@@ -241,11 +252,11 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
             auto add = [&](float (&to)[8], float* mem, auto&& f) __attribute__((always_inline)) {
                 if constexpr (R) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) to[j] += in ? f(j) : 0.0f;
+                    for (int j = 0; j < 8; ++j) to[j] += f(j);
                 } else {
                     float v[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = in ? f(j) : 0.0f;
+                    for (int j = 0; j < 8; ++j) v[j] = f(j);
                     collect(v, mem, true);
                 }
             };
@@ -460,11 +471,9 @@ hipError_t launch_join_bwd(const JoinArgs& a0, hipStream_t s) {
         else if (a.held == 2) hipLaunchKernelGGL((join_bwd_kernel<1, 2, true>), g, b, 0, s, a);
         else hipLaunchKernelGGL((join_bwd_kernel<1, 0, true>), g, b, 0, s, a);
     } else if (a.lpx == 64) {
-        if (a.held == 1) hipLaunchKernelGGL((join_bwd_kernel<64, 1, false>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((join_bwd_kernel<64, 2, false>), g, b, 0, s, a);
+        hipLaunchKernelGGL((join_bwd_kernel<64, 1, false>), g, b, 0, s, a);
     } else if (a.lpx == 16) {
         if (a.held == 1) hipLaunchKernelGGL((join_bwd_kernel<16, 1, false>), g, b, 0, s, a);
-        else if (a.held == 2) hipLaunchKernelGGL((join_bwd_kernel<16, 2, false>), g, b, 0, s, a);
         else hipLaunchKernelGGL((join_bwd_kernel<16, 0, false>), g, b, 0, s, a);
     } else {
         if (a.held == 1) hipLaunchKernelGGL((join_bwd_kernel<4, 1, false>), g, b, 0, s, a);

@@ -25,16 +25,16 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
     uint32_t wx[H][32];
     auto load_y = [&](int i, int cb) __attribute__((always_inline)) {
         uint32_t w[32];
-        load_raw<false>(w, a.y, a.qm, p, cb * 32, a.C);
-        raw_values<false>(v[i], w, a.y, cb * 32, a.C);
+        load_raw(w, a.y, p, cb * 32, a.C);
+        raw_values(v[i], w, a.y, cb * 32, a.C);
     };
     if constexpr (R) {
         uint32_t wy[H][32];
         each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) {
-            load_raw<false>(wy[i], a.y, a.qm, p, cb * 32, a.C);
-            if (a.x.p) load_raw<false>(wx[i], a.x, a.qm, p, cb * 32, a.C);
+            load_raw(wy[i], a.y, p, cb * 32, a.C);
+            if (a.x.p) load_raw(wx[i], a.x, p, cb * 32, a.C);
         });
-        each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) { raw_values<false>(v[i], wy[i], a.y, cb * 32, a.C); });
+        each_block<R>(a, l, [&](int i, int cb) __attribute__((always_inline)) { raw_values(v[i], wy[i], a.y, cb * 32, a.C); });
     }
     // mean and 1 / deviation of what `form` leaves in v
     auto moments = [&](const JoinNorm& k, int at, float& mu, float& r, auto&& form) __attribute__((always_inline)) {
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
         const int c0 = cb * 32;
         if constexpr (!R) {
             load_y(0, cb);
-            if (a.x.p) load_raw<false>(wx[0], a.x, a.qm, p, c0, a.C);
+            if (a.x.p) load_raw(wx[0], a.x, p, c0, a.C);
         }
         if (a.post.kind) {
             float g[32], b[32];
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
         }
         float f[32], x[32];
         load_factor<LPX>(f, a, p, c0);
-        if (a.x.p) raw_values<false>(x, wx[i], a.x, c0, a.C);
+        if (a.x.p) raw_values(x, wx[i], a.x, c0, a.C);
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[i][j] = fmaf(v[i][j], f[j], a.x.p ? x[j] : 0.0f);
         if (c0 + 32 > a.C) {
@@ -130,12 +130,13 @@ __global__ __launch_bounds__(512) void join_fwd_kernel(JoinArgs a) {
     });
 }
 
-// Rows of channels: eight channels a lane, a row's lanes next to each other.
-template <int LPX, int R>
-__global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
+// Rows of channels (CL), a row's lanes next to each other, and planes of few channels: eight
+// channels a lane.
+template <int LPX, int R, bool CL>
+__global__ __launch_bounds__(512) void join_eights_fwd_kernel(JoinArgs a) {
     constexpr int H = R ? R : 1;
     __shared__ float red[4][1][kJoinWaves * LPX];
-    const JoinLane l = join_lane<LPX, true>(a);
+    const JoinLane l = join_lane<LPX, CL>(a);
     const int wg = int(blockIdx.y * gridDim.x + blockIdx.x);
     if (wg >= a.grid) return;
     const int m = (wg * a.pg + l.pg) * LPX + l.px;
@@ -144,15 +145,15 @@ __global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
     float v[H][8];
     u32x8 wx[H];
     auto load_y = [&](int i, int e) __attribute__((always_inline)) {
-        values8<true>(v[i], load8<true>(a.y, a.qm, p, 8 * e, a.C), a.y, 8 * e, a.C);
+        values8<CL>(v[i], load8<CL>(a.y, a.qm, p, 8 * e, a.C), a.y, 8 * e, a.C);
     };
     if constexpr (R) {
         u32x8 wy[H];
         each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) {
-            wy[i] = load8<true>(a.y, a.qm, p, 8 * e, a.C);
-            if (a.x.p) wx[i] = load8<true>(a.x, a.qm, p, 8 * e, a.C);
+            wy[i] = load8<CL>(a.y, a.qm, p, 8 * e, a.C);
+            if (a.x.p) wx[i] = load8<CL>(a.x, a.qm, p, 8 * e, a.C);
         });
-        each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) { values8<true>(v[i], wy[i], a.y, 8 * e, a.C); });
+        each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) { values8<CL>(v[i], wy[i], a.y, 8 * e, a.C); });
     }
     // mean and 1 / deviation of what `form` leaves in v
     auto moments = [&](const JoinNorm& k, int at, float& mu, float& r, auto&& form) __attribute__((always_inline)) {
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[0] += v[i][j];
             });
-            lane_sum<LPX, true>(s, a, l, red[at]);
+            lane_sum<LPX, CL>(s, a, l, red[at]);
             mu = s[0] * a.invC;
             s[0] = 0;
         }
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
                 s[0] = fmaf(d, d, s[0]);
             }
         });
-        lane_sum<LPX, true>(s, a, l, red[at + 1]);
+        lane_sum<LPX, CL>(s, a, l, red[at + 1]);
         r = 1.0f / sqrtf(s[0] * a.invC + k.eps);
         if (a.stat && in && l.unit == 0) {
             a.stat[int64_t(at) * a.px.M + m] = mu;
@@ -192,19 +193,19 @@ __global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
         const int c0 = 8 * e;
         if constexpr (!R) {
             load_y(0, e);
-            if (a.x.p) wx[0] = load8<true>(a.x, a.qm, p, c0, a.C);
+            if (a.x.p) wx[0] = load8<CL>(a.x, a.qm, p, c0, a.C);
         }
         if (a.post.kind) {
             float g[8], b[8];
-            params8<false>(g, a.post.gamma, c0, a.C, 1.0f);
-            params8<false>(b, a.post.beta, c0, a.C, 0.0f);
+            params8<LPX == 64>(g, a.post.gamma, c0, a.C, 1.0f);
+            params8<LPX == 64>(b, a.post.beta, c0, a.C, 0.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = fmaf(g[j], (v[i][j] - mu1) * r1, b[j]);
         }
         float f[8], k[8], x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         keep8(k, a.drop, dp, e);
-        factor8<false>(f, a, p, c0);
-        if (a.x.p) values8<true>(x, wx[i], a.x, c0, a.C);
+        factor8<LPX == 64>(f, a, p, c0);
+        if (a.x.p) values8<CL>(x, wx[i], a.x, c0, a.C);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = fmaf(dropped(v[i][j], k[j]), f[j], x[j]);
         clear8(v[i], c0, a.C);
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
     if constexpr (R) each_eight<R>(a, l, join);
     float mu2 = 0, r2 = 0;
     if (a.pre.kind) moments(a.pre, 2, mu2, r2, join);
-    if (a.q) {       // the four lanes of a block of 32 channels together, also those past the last eight
+    if (CL && a.q) { // the four lanes of a block of 32 channels together, also those past the last eight
         for (int i = 0, e = l.unit; e < a.blocks * 4; e += l.ng, ++i) {
             float o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             if (8 * e < a.C) {
@@ -228,37 +229,38 @@ __global__ __launch_bounds__(512) void join_rows_fwd_kernel(JoinArgs a) {
     each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) {
         const int c0 = 8 * e;
         if constexpr (!R) join(0, e);
-        if (in) store8<true>(a.o, p, c0, a.C, v[i]);
+        if (in) store8<CL>(a.o, p, c0, a.C, v[i]);
         if (a.pre.kind && a.u.p) {
             float g[8], b[8];
-            params8<false>(g, a.pre.gamma, c0, a.C, 1.0f);
-            params8<false>(b, a.pre.beta, c0, a.C, 0.0f);
+            params8<LPX == 64>(g, a.pre.gamma, c0, a.C, 1.0f);
+            params8<LPX == 64>(b, a.pre.beta, c0, a.C, 0.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] = fmaf(g[j], (v[i][j] - mu2) * r2, b[j]);
-            if (in) store8<true>(a.u, p, c0, a.C, g);
+            if (in) store8<CL>(a.u, p, c0, a.C, g);
         }
     });
 }
 
-// Planes, forward: as the layer norm's (norm_fwd.hip), 32 channels a lane, 64 pixels a wave, or
-// 16 where there are few or many channels.  The others: eight channels a lane.  Rows: as many
-// lanes as a row has eights, up to 64, then up to eight waves, then two eights a lane.
-// Planes, backward: 64 pixels a wave, fewer where there are few, or more channels than eight
-// waves hold.
+// Rows of channels: eight channels a lane, as many lanes as a row has eights, up to 64, then up to
+// eight waves, then two eights a lane.  Planes, backward: 16 pixels a wave and four eights side by
+// side, 64 and one where there are three eights at most (4 x 64 x 256 x 256: two waves of 16
+// pixels 96 us, eight of 64, which meet at a barrier twice a step, 101), 4 where there are more than
+// 256 channels.  Planes, forward: up to three eights likewise (2 x 8 x 16 x 16 fp32 8 us, in lanes of 32
+// channels 13); else as the layer norm's (norm_fwd.hip), 32 channels a lane, 64 pixels a
+// wave, or 16 where there are few or many channels.
 void join_plan(JoinArgs& a, bool backward) {
     a.blocks = (a.C + 31) / 32;
     a.invC = 1.0f / float(a.C);
     const int eights = (a.C + 7) / 8;
     const int64_t M = a.px.M, waves = (M + 63) / 64 * a.blocks;
-    if (a.cl) {
-        int u = 4;
-        while (u < eights && u < 64) u *= 2;
-        a.lpx = 64 / u;
-        a.held = eights <= 8 * u ? 1 : eights <= 16 * u ? 2 : 0;
-        a.nw = std::min((eights + u * std::max(a.held, 1) - 1) / (u * std::max(a.held, 1)), kJoinWaves);
-    } else if (backward) {
-        a.lpx = eights <= 16 && waves >= 1024 ? 64 : eights <= 64 ? 16 : 4;
-        if (eights > 256) a.lpx = 16;
+    a.eights = a.cl || backward || (eights <= 3 && !a.q);
+    if (a.eights) {
+        if (a.cl) {
+            a.lpx = 16;
+            while (64 / a.lpx < eights && a.lpx > 1) a.lpx /= 2;
+        } else {
+            a.lpx = eights <= 3 ? 64 : eights <= 32 || eights > 256 ? 16 : 4;
+        }
         const int u = 64 / a.lpx;
         a.held = eights <= 8 * u ? 1 : eights <= 16 * u ? 2 : 0;
         a.nw = std::min((eights + u * std::max(a.held, 1) - 1) / (u * std::max(a.held, 1)), kJoinWaves);
@@ -282,7 +284,7 @@ void join_plan(JoinArgs& a, bool backward) {
     // Units: slices of a sample's groups.  Workgroups take them in turns; of one to four times as
     // many units as workgroups, what leaves the least idle.
     const int64_t all = int64_t(a.groups) * a.samples;
-    a.pg = int(std::max<int64_t>(1, std::min<int64_t>(std::max(1, 4 / a.nw), (all + 511) / 512)));
+    a.pg = int(std::max<int64_t>(1, std::min<int64_t>(std::max(1, (a.cl ? 8 : 4) / a.nw), (all + 511) / 512)));
     a.grid = int(std::min<int64_t>((all + a.pg - 1) / a.pg, 256 * std::clamp(8 / (a.nw * a.pg), 1, 4)));
     const int most = (a.groups + a.pg - 1) / a.pg;
     a.slices = std::min(a.grid, most);
@@ -305,13 +307,15 @@ hipError_t launch_join_fwd(const JoinArgs& a, hipStream_t s) {
     const unsigned x = unsigned(std::min(a.grid, 1 << 22));     // threads of a dimension: 32 bits
     const dim3 g(x, (unsigned(a.grid) + x - 1) / x), b(64 * a.nw * a.pg);
     if (a.cl) {
-        if (a.lpx == 16) hipLaunchKernelGGL((join_rows_fwd_kernel<16, 1>), g, b, 0, s, a);
-        else if (a.lpx == 8) hipLaunchKernelGGL((join_rows_fwd_kernel<8, 1>), g, b, 0, s, a);
-        else if (a.lpx == 4) hipLaunchKernelGGL((join_rows_fwd_kernel<4, 1>), g, b, 0, s, a);
-        else if (a.lpx == 2) hipLaunchKernelGGL((join_rows_fwd_kernel<2, 1>), g, b, 0, s, a);
-        else if (a.held == 1) hipLaunchKernelGGL((join_rows_fwd_kernel<1, 1>), g, b, 0, s, a);
-        else if (a.held == 2) hipLaunchKernelGGL((join_rows_fwd_kernel<1, 2>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((join_rows_fwd_kernel<1, 0>), g, b, 0, s, a);
+        if (a.lpx == 16) hipLaunchKernelGGL((join_eights_fwd_kernel<16, 1, true>), g, b, 0, s, a);
+        else if (a.lpx == 8) hipLaunchKernelGGL((join_eights_fwd_kernel<8, 1, true>), g, b, 0, s, a);
+        else if (a.lpx == 4) hipLaunchKernelGGL((join_eights_fwd_kernel<4, 1, true>), g, b, 0, s, a);
+        else if (a.lpx == 2) hipLaunchKernelGGL((join_eights_fwd_kernel<2, 1, true>), g, b, 0, s, a);
+        else if (a.held == 1) hipLaunchKernelGGL((join_eights_fwd_kernel<1, 1, true>), g, b, 0, s, a);
+        else if (a.held == 2) hipLaunchKernelGGL((join_eights_fwd_kernel<1, 2, true>), g, b, 0, s, a);
+        else hipLaunchKernelGGL((join_eights_fwd_kernel<1, 0, true>), g, b, 0, s, a);
+    } else if (a.eights) {
+        hipLaunchKernelGGL((join_eights_fwd_kernel<64, 1, false>), g, b, 0, s, a);
     } else if (a.lpx == 64) {
         if (a.held == 1) hipLaunchKernelGGL((join_fwd_kernel<64, 1>), g, b, 0, s, a);
         else hipLaunchKernelGGL((join_fwd_kernel<64, 2>), g, b, 0, s, a);
