@@ -196,12 +196,20 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
                 k = fetch_moments(m);
                 if constexpr (R > 1) each_eight<R>(a, l, [&](int i, int e) __attribute__((always_inline)) { fetch(w, i, p, e); });
             }
-            // lanes without a pixel hold another one's, with gradients of zero: nothing for the sums
-            if constexpr (R != 0) {
+            // lanes without a pixel have read another one's, maybe after its results were stored over it:
+            // zeros instead, which add nothing to the sums
+            auto clear = [&](int i) __attribute__((always_inline)) {
+                const u32x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
                 if (!__all(in)) {
-#pragma unroll
-                    for (int i = 0; i < H; ++i) w.d[i] = in ? w.d[i] : u32x8{0, 0, 0, 0, 0, 0, 0, 0}, w.r[i] = in ? w.r[i] : u32x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    w.o[i] = in ? w.o[i] : zero;
+                    w.d[i] = in ? w.d[i] : zero;
+                    w.y[i] = in ? w.y[i] : zero;
+                    w.r[i] = in ? w.r[i] : zero;
                 }
+            };
+            if constexpr (R != 0) {
+#pragma unroll
+                for (int i = 0; i < H; ++i) clear(i);
             }
             const float mu1 = k.mu1, r1 = k.r1, mu2 = k.mu2, r2 = k.r2;
             DropPixel dp{};
@@ -216,7 +224,7 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
                 const int c0 = 8 * e;
                 if constexpr (!R) {
                     fetch(w, 0, p, e);
-                    w.d[0] = in ? w.d[0] : u32x8{0, 0, 0, 0, 0, 0, 0, 0}, w.r[0] = in ? w.r[0] : u32x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    clear(0);
                 }
                 {
                     const JoinArgs& b = fresh();

@@ -377,7 +377,8 @@ def test_join(shape, layout, name):
 # channels for the registers, gates of a sample a row and of more samples than walkers
 JOIN_SIZES = [((1, 40, 300, 231), "gaps"), ((3, 64, 160, 161), "dense"), ((2, 300, 121, 61), "padded"), ((1, 512, 120, 101), "dense"),
               ((5, 24, 209, 111), "dense"), ((1100, 40, 3, 2), "dense"), ((3000, 100, 1, 1), "rows"), ((37, 520, 45, 1), "slice"),
-              ((5, 4104, 40, 1), "rows"), ((2, 1056, 30, 33), "dense"), ((2500, 1, 1, 1), "rows")]
+              ((5, 4104, 40, 1), "rows"), ((2, 1056, 30, 33), "dense"), ((2500, 1, 1, 1), "rows"), ((3, 8200, 21, 1), "rows"),
+              ((2, 8999, 4, 1), "slice"), ((2, 2300, 9, 40), "dense"), ((4, 20, 60, 61), "gaps")]
 
 
 @pytest.mark.parametrize("shape,layout", JOIN_SIZES, ids=str)
@@ -389,7 +390,8 @@ def test_join_sizes(shape, layout, name):
 def test_join_in_place_and_without_a_residual():
     """o over x, u over y, dx over d_o, dy over y, to the bit; no x is an x of zeros."""
     g = rng(9)
-    for shape, layout in (((2, 48, 9, 11), "dense"), ((3, 600, 7, 1), "rows"), ((1, 4200, 5, 1), "rows"), ((1, 1100, 4, 5), "dense")):
+    for shape, layout in (((2, 48, 9, 11), "dense"), ((3, 600, 7, 1), "rows"), ((1, 4200, 5, 1), "rows"), ((1, 1100, 4, 5), "dense"),
+                          ((2, 8300, 3, 1), "rows"), ((1, 2100, 4, 5), "gaps"), ((2, 20, 33, 35), "dense"), ((3, 200, 40, 41), "padded")):
         N, C, H, W = shape
         y, _ = put(layout, randn(g, *shape), "f32")
         x, _ = put(layout, randn(g, *shape), "f32")
