@@ -4,7 +4,10 @@
 // Bound: the weights, each read once: memory latency first.  As for the plain product
 // (linear_few.hip) a workgroup deals k out to sixteen waves, whose sums meet in LDS in order;
 // forward, eight channels a workgroup: eight rows of Wg and eight of Wu fill the matrix
-// instruction's sixteen.
+// instruction's sixteen.  Forward on up to 16 pixels with two workgroups or more a compute unit,
+// eight waves: one pixel, 1024 to twice 4096 in bf16, 6.4 us (16.8 MB: 3.4 at a copy's rate), with
+// sixteen 7.5; 2048 to twice 8192 14.5 (4.6 TB/s) and 17.6.  Backward (27.8 and 24.1) and below 512
+// workgroups (no difference) sixteen.
 #include <algorithm>
 
 #include "gate.h"
@@ -12,10 +15,10 @@
 
 namespace dc {
 
-template <typename T, bool BWD, bool CL, int NT>
-__global__ __launch_bounds__(64 * kFewWaves) void gate_few_kernel(GateArgs a, int M) {
+template <typename T, bool BWD, bool CL, int NT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void gate_few_kernel(GateArgs a, int M) {
     constexpr int CH = BWD ? 16 : 8;       // channels of a workgroup
-    __shared__ float sums[kFewWaves][NT * 256];
+    __shared__ float sums[WAVES][NT * 256];
     const LinearArgs& l = a.l;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int o0 = blockIdx.x * CH, m0 = blockIdx.y * NT * 16;
@@ -24,7 +27,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void gate_few_kernel(GateArgs a, in
     if constexpr (BWD) row = min(o0 + (lane & 15), l.rows - 1);
     else row = min(o0 + (lane & 7), l.rows - 1) + (lane & 8 ? l.rows : 0);
     few_sums<T, BWD, CL, NT>(sums, l, row, m0, M, hw, lane, wave);
-    for (int e = threadIdx.x; e < NT * 16 * CH; e += 64 * kFewWaves) {
+    for (int e = threadIdx.x; e < NT * 16 * CH; e += 64 * WAVES) {
         const int in = e % (16 * CH), t = e / (16 * CH);
         // channels next to each other in memory (rows of channels) lie next to each other on the lanes
         const int ch = CL ? in % CH : in / 16, mt = CL ? in / CH : in % 16;
@@ -34,7 +37,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void gate_few_kernel(GateArgs a, in
         const int n = m / hw, pix = m - n * hw;
         float v = 0, u[1] = {0};
 #pragma unroll
-        for (int i = 0; i < kFewWaves; ++i) v += sums[i][at];
+        for (int i = 0; i < WAVES; ++i) v += sums[i][at];
         auto index = [&](const View& w, int c) __attribute__((always_inline)) {
             const int r = pix / l.s.len;
             return n * w.sn + r * w.sh + (pix - r * l.s.len) + c * w.sc;
@@ -72,7 +75,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void gate_few_kernel(GateArgs a, in
             if (l.h.dt >= 0) put(l.h, o, stays ? f[0] * zu * factor : 0.0f);
         } else {
 #pragma unroll
-            for (int i = 0; i < kFewWaves; ++i) u[0] += sums[i][at + 128];
+            for (int i = 0; i < WAVES; ++i) u[0] += sums[i][at + 128];
             float f[1] = {v};
             if (l.bias) {
                 f[0] += l.bias[o];
@@ -100,9 +103,15 @@ template <typename T, bool BWD, bool CL>
 static void launch(const GateArgs& a, int M, hipStream_t s) {
     const int ch = BWD ? 16 : 8;
     const dim3 g((a.l.rows + ch - 1) / ch, (M + 63) / 64), t(64 * kFewWaves);
-    if (M <= 16) hipLaunchKernelGGL((gate_few_kernel<T, BWD, CL, 1>), g, t, 0, s, a, M);
-    else if (M <= 32) hipLaunchKernelGGL((gate_few_kernel<T, BWD, CL, 2>), g, t, 0, s, a, M);
-    else hipLaunchKernelGGL((gate_few_kernel<T, BWD, CL, 4>), g, t, 0, s, a, M);
+    if constexpr (!BWD) {
+        if (M <= 16 && g.x >= 512) {
+            hipLaunchKernelGGL((gate_few_kernel<T, BWD, CL, 1, 8>), g, dim3(64 * 8), 0, s, a, M);
+            return;
+        }
+    }
+    if (M <= 16) hipLaunchKernelGGL((gate_few_kernel<T, BWD, CL, 1, kFewWaves>), g, t, 0, s, a, M);
+    else if (M <= 32) hipLaunchKernelGGL((gate_few_kernel<T, BWD, CL, 2, kFewWaves>), g, t, 0, s, a, M);
+    else hipLaunchKernelGGL((gate_few_kernel<T, BWD, CL, 4, kFewWaves>), g, t, 0, s, a, M);
 }
 
 template <typename T, bool BWD>

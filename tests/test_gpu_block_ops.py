@@ -227,6 +227,17 @@ def test_gate_blocks(name, types):
     check_gate(*GATE_BLOCKS[name], *types)
 
 
+# up to 16 pixels of many channels: k that ends with a whole group of steps, a step, part of one, and that one group holds
+GATE_FEW = [((1, 1000, 1, 1, 4104), "rows"), ((3, 200, 2, 2, 4100), "dense"), ((16, 70, 1, 1, 4099), "slice"), ((7, 2048, 1, 1, 4096), "rows"),
+            ((1, 31, 3, 5, 4111), "gaps"), ((33, 1056, 1, 1, 72), "rows"), ((1, 1, 1, 1, 4096), "rows"), ((50, 96, 1, 1, 1), "rows")]
+
+
+@pytest.mark.parametrize("shape,layout", GATE_FEW, ids=str)
+@pytest.mark.parametrize("types", GATE_TYPES, ids=str)
+def test_gate_few(shape, layout, types):
+    check_gate(shape, layout, *types)
+
+
 def test_gate_without_bias_in_mixed_layouts():
     g = rng(6)
     for lx, lh in (("rows", "dense"), ("dense", "rows"), ("slice", "gaps")):
