@@ -512,9 +512,10 @@ dc_status dc_join_fwd(const dc_view* vy, const void* y, const dc_norm* post, con
  * o is NULL, read as it was stored, in its type's precision, and x is not looked at.  y is needed
  * where o is formed, where there is a post norm and where a gradient of scale or gate is wanted, else
  * it may be NULL.  y, x and o may be in 8 bits (DC_Q8).  stat is what the forward pass wrote.  dx
- * may be NULL.  grads (NULL: none): fp32, [C] each and [N][C] for gate; NULL where not wanted, and
- * for parameters that the call does not have.  accumulate = 0 overwrites them, 1 adds to them.  dx
- * may be d_o, dy may be y or du (same view and type).  workspace: at least
+ * may be NULL.  grads (NULL: none): fp32, [C] each and [N][C] for gate; NULL where not wanted, and for
+ * a gate, a pre or a post norm that the call does not have (DC_ERR_ARG); scale, gamma and beta that
+ * are NULL, 1 or 0, have a gradient all the same.  accumulate = 0 overwrites them, 1 adds to them.
+ * dx may be d_o, dy may be y or du (same view and type); nothing else overlaps.  workspace: at least
  * dc_join_bwd_workspace_bytes(vdy, whether there is a gate) bytes, if there are grads.  The
  * summation order is fixed.
  */

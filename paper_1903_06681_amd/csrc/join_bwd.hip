@@ -11,6 +11,9 @@
 // lane keeps to its eight channels, so that the sums over pixels are its own until a workgroup's
 // end (40 registers; 32 channels a lane left no room for them, and 160 values a wave's 64 pixels
 // to halve across its lanes).  A second launch adds the workgroups' sums in order.  No atomics.
+// Two waves a SIMD: 4 x 64 x 256 x 256 with fp32 x 95 us (3.2 TB/s), 8192 rows of 1024 bf16 46 (2.3);
+// neither barriers of fewer waves (two a workgroup: 47), nor stores put off until the next
+// step's loads are issued (45.5), nor two eights a lane (no barrier, but scratch: 67) change that much.
 #include <algorithm>
 
 #include "join.h"
