@@ -6,8 +6,10 @@
 // forward, eight channels a workgroup: eight rows of Wg and eight of Wu fill the matrix
 // instruction's sixteen.  Forward on up to 16 pixels with two workgroups or more a compute unit,
 // eight waves: one pixel, 1024 to twice 4096 in bf16, 6.4 us (16.8 MB: 3.4 at a copy's rate), with
-// sixteen 7.5; 2048 to twice 8192 14.5 (4.6 TB/s) and 17.6.  Backward (27.8 and 24.1) and below 512
-// workgroups (no difference) sixteen.
+// sixteen 7.5; 2048 to twice 8192 14.5 (4.6 TB/s) and 17.6.  Backward and below 512 workgroups
+// (no difference) sixteen.  Backward, a workgroup reads 32 or 64 bytes of a weight row: those that
+// read the rest of a line run on the same XCD, whose L2 has it by then (one pixel, 2048 from 8192 in
+// bf16, with the product's gradient in turn: 9.5 us, dealt out over the XCDs 23.6).
 #include <algorithm>
 
 #include "gate.h"
@@ -21,7 +23,7 @@ __global__ __launch_bounds__(64 * WAVES) void gate_few_kernel(GateArgs a, int M)
     __shared__ float sums[WAVES][NT * 256];
     const LinearArgs& l = a.l;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int o0 = blockIdx.x * CH, m0 = blockIdx.y * NT * 16;
+    const int o0 = (BWD ? xcd_range(blockIdx.x, gridDim.x) : int(blockIdx.x)) * CH, m0 = blockIdx.y * NT * 16;
     const int hw = int(l.s.dsample.d) / l.s.cpr * l.s.len;
     int row;
     if constexpr (BWD) row = min(o0 + (lane & 15), l.rows - 1);
