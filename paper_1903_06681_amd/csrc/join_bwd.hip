@@ -97,19 +97,19 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
         });
         __syncthreads();
     }
-    const int turns = (a.units + a.grid - 1) / a.grid, per = a.slices * a.pg, steps = (a.groups + per - 1) / per;
+    const int per = a.slices * a.pg, steps = (a.groups + per - 1) / per;
     int par = 0;
-    // every wave takes the same number of turns and steps: barriers
-    for (int turn = 0; turn < turns; ++turn) {
-        const int unit = wg + turn * a.grid, uu = min(unit, a.units - 1);
-        const int smp = int(a.dslices.div(uint32_t(uu))), slice = uu - smp * a.slices;
-        float* const spart = a.spart + int64_t(uu) * width;
+    // Every wave of a workgroup takes the same units and steps (barriers); a unit's sums are written by
+    // the workgroup that takes it and by no other, so one without a unit in the last turn does nothing there.
+    for (int unit = wg; unit < a.units; unit += a.grid) {
+        const int smp = int(a.dslices.div(uint32_t(unit))), slice = unit - smp * a.slices;
+        float* const spart = a.spart + int64_t(unit) * width;
 #pragma unroll
         for (int i = 0; i < H; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) tacc[i][j] = 0;
         if constexpr (!R) {
-            if (want_scale && unit < a.units)
+            if (want_scale)
                 each_eight<R>(a, l, [&](int, int e) {
                     for (int j = 0; j < 8; ++j) spart[8 * e + j] = 0;
                 });
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
         // where step st's pixel lies (a valid one's place where there is none)
         auto place = [&](int st, bool& in, int& m) __attribute__((always_inline)) {
             const int64_t q = (int64_t(slice + st * a.slices) * a.pg + l.pg) * LPX + l.px;
-            in = unit < a.units && q < a.span;
+            in = q < a.span;
             const JoinArgs& b = fresh();
             m = int(smp * int64_t(b.span) + min(q, int64_t(b.span) - 1));
             return pixel_of(b.px, m);
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(512, 2) void join_bwd_kernel(JoinArgs) {
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
                     const int e = l.unit + i * l.ng;
-                    collect(tacc[i], spart + 8 * e, unit < a.units && 8 * e < a.C);
+                    collect(tacc[i], spart + 8 * e, 8 * e < a.C);
                 }
             }
         }
