@@ -231,7 +231,7 @@ dc_status dc_join_bwd(const dc_view* vdu, const void* du, const dc_view* vdo, co
     JoinArgs a;
     std::memset(&a, 0, sizeof(a));
     if ((st = join_norm(post, &a.post)) != DC_OK) return st;
-    if ((st = join_norm(pre, &a.pre)) != DC_OK) return st;
+    if ((st = join_norm(du ? pre : nullptr, &a.pre)) != DC_OK) return st;    // without du none: its parameters are not read
     if (du && !a.pre.kind) return DC_ERR_ARG;
     static const dc_join_grads none = {};
     const dc_join_grads& g = grads ? *grads : none;
