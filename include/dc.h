@@ -462,7 +462,8 @@ dc_status dc_dropout(const dc_drop* drop, const dc_view* vx, const void* x, cons
  * w is [2K][C], Wg then Wu, of x's type; bias fp32 [2K], bg then bu, or NULL; drop NULL: none.
  * zg and zu are written too unless both are NULL, for dc_gate_bwd_data: two tensors of one
  * view (K channels), whole (fp32, bf16) or in 8 bits (DC_Q8).  K = vh->C; h is fp32 or bf16.
- * Numbers are dc_linear_fwd's: the act DC_ACT_NONE takes zg itself.
+ * Numbers are dc_linear_fwd's: the act DC_ACT_NONE takes zg itself.  As there, the order of a sum is the
+ * same for every pixel of a call.
  */
 dc_status dc_gate_fwd(const dc_view* vx, const void* x, const void* w, const float* bias, int32_t act, const dc_drop* drop,
                       const dc_view* vz, void* zg, void* zu, const dc_view* vh, void* h, void* stream);

@@ -317,10 +317,13 @@ __global__ __launch_bounds__(S::TH, S::OCC) void gate_kernel(GateArgs a) {
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-    // workgroups start at different slices: rows lie a power of two apart, and the same slice of all
-    // of them on few of L2's channels (501 us and 483 for 65536 rows, 512 to twice 2048)
+    // Blocks of different channels start at different slices: rows lie a power of two apart, and the same
+    // slice of all of them on few of L2's channels (forward, all from the first one and so: 65536 rows of
+    // 512 to twice 2048 439 us and 424, 8 x 112 x 112 of 256 to twice 1024 279 and 246, its gradient 344 and
+    // 336; 8192 rows of 1024 to twice 4096 169 and 171).  By their channels, not by their pixels too (the
+    // same times): the order of a sum, and with it its last bits, does not change with a pixel's place.
     tile_loop<S, AK, PK, DIRECT>(acc, sa, sb, l.a, l.b, l.s, 0, l.a.red, lds, row0, col0, lane, [](int, const uint4&) {},
-                                 (tr + tc) % ((l.a.red + S::BK - 1) / S::BK));
+                                 tr % ((l.a.red + S::BK - 1) / S::BK));
 
     // As the plain product's: a wave's blocks pass through its share of LDS, both sums of a
     // channel together, and the epilogue is one loop.
