@@ -29,8 +29,8 @@ __device__ __forceinline__ int64_t few_offset(const Slots& s, int hw, int m, con
 }
 
 // The waves' sums of a block: 16 rows (row: the lane's, of lane % 16) by NT tiles of 16 pixels
-// from m0 on.  BWD: weights [k][row].
-template <typename T, bool BWD, bool CL, int NT, int WAVES>
+// from m0 on.  BWD: weights [k][row].  DEEP: whole steps of k several at once.
+template <typename T, bool BWD, bool CL, int NT, int WAVES, bool DEEP = true>
 __device__ __forceinline__ void few_sums(float (&sums)[WAVES][NT * 256], const LinearArgs& a, int row, int m0, int M, int hw,
                                          int lane, int wave) {
     constexpr int E = 16 / int(sizeof(T)), STEP = 4 * E;      // k of a lane's chunk, of a wave's step
@@ -96,8 +96,11 @@ __device__ __forceinline__ void few_sums(float (&sums)[WAVES][NT * 256], const L
         }
     };
     int s = s0;
-    some(std::integral_constant<int, NT == 4 ? 2 : 4>{}, s);
-    if constexpr (NT != 4) some(std::integral_constant<int, 2>{}, s);
+    if constexpr (DEEP) {
+        some(std::integral_constant<int, NT == 4 ? 2 : 4>{}, s);
+        if constexpr (NT != 4) some(std::integral_constant<int, 2>{}, s);
+    }
+#pragma unroll(DEEP ? 1 : 4)
     for (; s < s1; ++s) {
         const int k = s * STEP + (lane >> 4) * E, n = red - k, kk = min(k, red - 1);
         uint4 fa = make_uint4(0, 0, 0, 0), fb[NT];

@@ -15,15 +15,15 @@
 
 namespace dc {
 
-// NT: tiles of 16 pixels.  BWD: weights [k][row], and the activation's slope.
-template <typename T, bool BWD, bool CL, int NT>
+// NT: tiles of 16 pixels.  BWD: weights [k][row], and the activation's slope.  DEEP: see deep_pays.
+template <typename T, bool BWD, bool CL, int NT, bool DEEP>
 __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a, int M) {
     __shared__ float sums[kFewWaves][NT * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int o0 = (BWD ? xcd_range(blockIdx.x, gridDim.x) : int(blockIdx.x)) * 16, m0 = blockIdx.y * NT * 16;
     const int hw = int(a.s.dsample.d) / a.s.cpr * a.s.len;
     const int row = min(o0 + (lane & 15), a.rows - 1);
-    few_sums<T, BWD, CL, NT>(sums, a, row, m0, M, hw, lane, wave);
+    few_sums<T, BWD, CL, NT, kFewWaves, DEEP>(sums, a, row, m0, M, hw, lane, wave);
     // channels next to each other in memory (rows of channels) lie next to each other on the lanes
     for (int e = threadIdx.x; e < NT * 256; e += 64 * kFewWaves) {
         const int in = e & 255, o = o0 + (CL ? in & 15 : in >> 4), mt = CL ? in >> 4 : in & 15, m = m0 + (e >> 8) * 16 + mt;
@@ -78,12 +78,40 @@ bool linear_few(const LinearArgs& a, bool bwd, bool f32) {
     return M <= 64 || (a.a.red >= 256 && (a.rows + 63) / 64 * ((M + 63) / 64) <= limit);
 }
 
+// Whether a wave's steps of k (per of them) go out several at once, in up to 128 registers, or one after the
+// other as the compiler arranges them, in about half.  us, several at once against one after the other:
+//   one step a wave: nothing to gain, and the longer code costs (64 to 1000 channels, 48 pixels, fp32 4.8
+//     against 4.1; 512 to 16384, 24 pixels, bf16 13.4 and 11.7)
+//   from two steps on: one pixel, 4096 to 4096, bf16 9.0 and 11.4, fp32 14.0 and 18.5; 64 pixels, 1024 to
+//     1024, rows, fp32 13.8 and 15.9; 24 pixels, planes, bf16 6.4 and 7.4
+//   more workgroups than compute units where it takes the registers of a second one: gradient of 24 rows,
+//     1024 to 8192, bf16 11.9 and 10.0, 1536 to 8192 15.2 and 13.0; 24 rows, 512 to 16384, fp32 20.4 and
+//     18.4 (sums over 4096 the same within 5%)
+//   fp32 planes, two tiles or four, whose loads are 4 bytes each: 768 to 1024, 64 pixels 10.2 and 10.3,
+//     4096 to 1024 44 and 38; gradient 768 to 4096 9.9 and 11.1, 1024 to 2048 10.4 and 12.5, to 4096 15.0 and 13.8
+template <typename T, bool BWD, bool CL, int NT>
+static bool deep_pays(int per, int64_t workgroups) {
+    constexpr bool f32 = sizeof(T) == 4;
+    constexpr bool second = f32 ? NT == 2 || (NT == 4 && CL) : NT < 4 && (BWD || !CL);
+    if (per < 2 || (second && workgroups > 256)) return false;
+    return !f32 || CL || NT == 1 || per <= 3 || (BWD && per == 4 && workgroups <= 128);
+}
+
+template <typename T, bool BWD, bool CL, int NT>
+static void launch(const LinearArgs& a, int M, dim3 g, hipStream_t s) {
+    const int steps = (a.a.red + 64 / int(sizeof(T)) - 1) / (64 / int(sizeof(T))), per = (steps + kFewWaves - 1) / kFewWaves;
+    if (deep_pays<T, BWD, CL, NT>(per, int64_t(g.x) * g.y))
+        hipLaunchKernelGGL((linear_few_kernel<T, BWD, CL, NT, true>), g, dim3(64 * kFewWaves), 0, s, a, M);
+    else
+        hipLaunchKernelGGL((linear_few_kernel<T, BWD, CL, NT, false>), g, dim3(64 * kFewWaves), 0, s, a, M);
+}
+
 template <typename T, bool BWD, bool CL>
 static void launch(const LinearArgs& a, int M, hipStream_t s) {
-    const dim3 g((a.rows + 15) / 16, (M + 63) / 64), t(64 * kFewWaves);
-    if (M <= 16) hipLaunchKernelGGL((linear_few_kernel<T, BWD, CL, 1>), g, t, 0, s, a, M);
-    else if (M <= 32) hipLaunchKernelGGL((linear_few_kernel<T, BWD, CL, 2>), g, t, 0, s, a, M);
-    else hipLaunchKernelGGL((linear_few_kernel<T, BWD, CL, 4>), g, t, 0, s, a, M);
+    const dim3 g((a.rows + 15) / 16, (M + 63) / 64);
+    if (M <= 16) launch<T, BWD, CL, 1>(a, M, g, s);
+    else if (M <= 32) launch<T, BWD, CL, 2>(a, M, g, s);
+    else launch<T, BWD, CL, 4>(a, M, g, s);
 }
 
 template <typename T, bool BWD>
