@@ -18,6 +18,7 @@ namespace dc {
 struct FastDiv {
     uint32_t m, sh, d;
     __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) >> sh) + (m ? 0 : n); }   // no branch
+    __device__ __forceinline__ uint32_t div_branch(uint32_t n) const { return m ? __umulhi(n, m) >> sh : n; }
 };
 
 inline FastDiv fast_div(uint32_t d) {
@@ -179,14 +180,17 @@ __device__ __forceinline__ float q8_value(uint32_t w, int k, float step) {
     return float(int32_t(w << (24 - 8 * k)) >> 24) * step;
 }
 
-// Where pixel m of the numbering lies; the last one's place for m past it.
+// Where pixel m of the numbering lies; the last one's place for m past it.  BRANCH: divisions by
+// one apart, which the norm's gradient keeps its registers with (from an fp32 x in bf16 8 bytes of
+// scratch a lane, else 16: 32 x 64 x 56 x 56 22.5 us and 24.3, 32 x 256 x 28 x 28 27.3 and 28.5).
 struct Pixel { int n, h, w, pix; };
+template <bool BRANCH = false>
 __device__ __forceinline__ Pixel pixel_of(const Pixels& x, int m0) {
     Pixel r;
     const int m = min(m0, x.M - 1);
-    r.n = int(x.dHW.div(uint32_t(m)));
+    r.n = int(BRANCH ? x.dHW.div_branch(uint32_t(m)) : x.dHW.div(uint32_t(m)));
     r.pix = m - r.n * x.HW;
-    r.h = int(x.dlen.div(uint32_t(r.pix)));
+    r.h = int(BRANCH ? x.dlen.div_branch(uint32_t(r.pix)) : x.dlen.div(uint32_t(r.pix)));
     r.w = r.pix - r.h * x.len;
     return r;
 }

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(512, LPX == 64 && R == 1 ? 3 : 2) void norm_bwd_ker
         const int m = (g0 + l.pg) * LPX + l.px;
         const bool in = m < a.px.M;
         const int mm = min(m, a.px.M - 1);
-        const Pixel p = pixel_of(a.px, m);
+        const Pixel p = pixel_of<true>(a.px, m);
         const float mu = a.stat[mm], r = a.stat[int64_t(a.px.M) + mm];
         float vx[H][32], vd[H][32];
         auto load = [&](int i, int cb) __attribute__((always_inline)) {
