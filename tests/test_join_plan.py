@@ -7,8 +7,17 @@ import subprocess
 
 import pytest
 
-from test_act_sanitizers import CLANG, CSRC, HIPCC, ROOT, SAN, _run
 from test_gpu_join_units import UNITS
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SAN, CSRC = os.path.join(ROOT, "tests", "sanitize"), os.path.join(ROOT, "paper_1903_06681_amd", "csrc")
+HIPCC, CLANG = "/opt/rocm/bin/hipcc", "/opt/rocm/lib/llvm/bin/clang"
+
+
+def _run(cmd):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, (cmd[0], r.stdout[-3000:], r.stderr[-3000:])
+    return r
 
 
 @pytest.mark.skipif(not (os.path.exists(HIPCC) and os.path.exists(CLANG) and os.path.isdir(SAN)), reason="ROCm toolchain or sources missing")
