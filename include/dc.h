@@ -473,7 +473,8 @@ dc_status dc_gate_fwd(const dc_view* vx, const void* x, const void* w, const flo
  *   dh = drop(W2^T dy),  dz = (dh zu act'(zg), then dh act(zg)),
  * w is W2, [vdy->C][K] of dy's type, K = vz->C; dz has 2K channels, so that the first
  * product's gradients are dc_linear_bwd_data's and dc_linear_bwd_filter's of w as a [2K][C]
- * matrix.  h, drop(act(zg) zu) once more from what was kept, is written unless NULL.
+ * matrix.  h, drop(act(zg) zu) once more from what was kept, is written unless NULL.  As 2K channels
+ * are a view's, K is up to 2^19 here (forward 2^20, with 2 K C below 2^31).
  */
 dc_status dc_gate_bwd_data(const dc_view* vdy, const void* dy, const void* w, int32_t act, const dc_drop* drop,
                            const dc_view* vz, const void* zg, const void* zu, const dc_view* vh, void* h,

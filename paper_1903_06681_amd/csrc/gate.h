@@ -530,6 +530,16 @@ static void launch_gate_shape(GateArgs a, hipStream_t s) {
     else hipLaunchKernelGGL((gate_kernel<S, BWD, false, false>), g, t, 0, s, a);
 }
 
+// The large block takes sums over more than 128 where 256 x 256 results a compute unit are there (two
+// workgroups each forward, four backward).  us, large against middle, by sum, channels and pixels:
+//   forward  rows, bf16: 256 to 256 on 16384 (128 x 128 blocks of 256: middle) 18.3 and 14.7, on 32768 25 and 27;
+//            160 to 1024 on 8192 22 and 24, 192 22.4 and 21.5, 512 33 and 36, 1024 48 and 57, 128 20.4 and 20.2,
+//            64 17.4 and 16.3.  fp32: 192 on 8192 69 and 74, 512 145 and 156, 128 54 and 56, 64 39 and 37;
+//            1024 on 4096 (middle) 147 and 153.  Planes much as rows (fp32, 512 to 1024 on 4096, middle, 83 and 95).
+//   backward rows, bf16: 160 to 1024 on 16384 33.5 and 33.5, 512 47 and 46, 1024 66 and 67, on 32768 137 and 154;
+//            128 32 and 32; 1024 to 1024 on 8192 (middle) 35 and 39.  fp32: 192 on 16384 120 and 111, 512 184
+//            and 185, 1024 314 and 320.  Planes, bf16: 192 on 16384 63 and 57, 512 70 and 61, 1024 83 and 83, on
+//            32768 145 and 149: there the middle one would be the better up to sums over 512.
 template <typename T, bool BWD>
 static hipError_t launch_gate(const GateArgs& a, hipStream_t s) {
     const int64_t slots = int64_t(a.l.s.chunks) * a.l.s.per, rows = int64_t(a.l.rows) * (BWD ? 1 : 2);

@@ -10,8 +10,10 @@
 // first two as the forward pass formed it, before its rounding (or read, where it is given).  A
 // lane keeps to its eight channels, so that the sums over pixels are its own until a workgroup's
 // end (40 registers; 32 channels a lane left no room for them, and 160 values a wave's 64 pixels
-// to halve across its lanes).  A second launch adds the workgroups' sums in order.  No atomics.
-// Two waves a SIMD: 4 x 64 x 256 x 256 with fp32 x 95 us (3.2 TB/s), 8192 rows of 1024 bf16 46 (2.3);
+// to halve across its lanes).  A second launch adds the workgroups' sums in order.  No atomics.  What
+// does not fit the registers (R = 0) goes through its channels one eight at a time, three times, with the
+// sums in memory: 4096 rows of 8200 bf16 671 us, of 8192 (two eights a lane) 259.
+// Two waves a SIMD: 4 x 64 x 256 x 256 with fp32 x 92 us (3.3 TB/s), 8192 rows of 1024 bf16 44 (2.3);
 // neither barriers of fewer waves (two a workgroup: 47), nor stores put off until the next
 // step's loads are issued (45.5), nor two eights a lane (no barrier, but scratch: 67) change that much.
 #include <algorithm>

@@ -245,8 +245,9 @@ __global__ __launch_bounds__(512) void join_eights_fwd_kernel(JoinArgs a) {
 // Rows of channels: eight channels a lane, as many lanes as a row has eights, up to 64, then up to
 // eight waves, then two eights a lane.  Planes, backward: 16 pixels a wave and four eights side by
 // side, 64 and one where there are three eights at most (4 x 64 x 256 x 256: two waves of 16
-// pixels 96 us, eight of 64, which meet at a barrier twice a step, 101), 4 where there are more than
-// 256 channels.  Planes, forward: up to three eights likewise (2 x 8 x 16 x 16 fp32 8 us, in lanes of 32
+// pixels 96 us, eight of 64, which meet at a barrier twice a step, 101), 4 for 257 to 2048 channels.
+// Above that 16 again, and the eights one by one (held = 0: read again for every sum), as in rows of
+// more than 8192 channels.  Planes, forward: up to three eights likewise (2 x 8 x 16 x 16 fp32 8 us, in lanes of 32
 // channels 13); else as the layer norm's (norm_fwd.hip), 32 channels a lane, 64 pixels a
 // wave, or 16 where there are few or many channels.
 void join_plan(JoinArgs& a, bool backward) {
